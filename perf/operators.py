@@ -323,7 +323,7 @@ def prepare(case, seed):
         s["bias"] = None
         if case["bias"]:
             bias = torch.zeros((B, V), device=DEV)
-            at = torch.randint(0, V, (B, 300), device=DEV, generator=gen)
+            at = torch.rand((B, V), device=DEV, generator=gen).topk(300).indices      # 300 different tokens each
             s["bias"] = bias.scatter_(1, at, _normal(gen, (B, 300), torch.float32))
         s["masks"] = s["mask_index"] = None
         if case["masks"]:
