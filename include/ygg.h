@@ -13,6 +13,14 @@
  * ygg_prune_for_verification (verification-width pruning, Sec. 4.2), and ygg_debug_validate, which
  * reports the data-dependent contract violations that the three calls above do not check.
  *
+ * What a decode step needs beside them:
+ *
+ *   ygg_tree_rotary           rotary positions of a tree's (or a prompt's) queries and keys
+ *   ygg_tree_attention_block8 the verifier's attention over a cache in 8 bits with a scale per 64 tokens and head
+ *   ygg_block8_append         writes accepted (or prompt) tokens into that cache
+ *   ygg_constrain_logits      penalties, biases and grammar masks on logits, node by node, and their first maxima
+ *   ygg_count_tokens          the counts of confirmed tokens that the penalties go by
+ *
  * Conventions shared by every call
  *   - All tensor pointers are DEVICE pointers owned by the caller; the ygg_shape struct is HOST
  *     memory and is only read during the call.  The library never allocates, frees or keeps
@@ -61,11 +69,16 @@ typedef enum {
 typedef enum {
     YGG_F32 = 0,
     YGG_BF16 = 1,
-    YGG_FP8_E4M3 = 2   /* K and V (cache and tree) as 8-bit E4M3 codes, Q and O bf16; head_dim 128;
+    YGG_FP8_E4M3 = 2,  /* K and V (cache and tree) as 8-bit E4M3 codes, Q and O bf16; head_dim 128;
                           accepted by ygg_tree_attention_fp8kv and ygg_accept_and_compact only */
+    YGG_FP8_BLOCK = 3  /* the cache is a ygg_block8_cache, everything else is bf16; accepted by
+                          ygg_tree_attention_block8, ygg_block8_append and ygg_tree_rotary */
 } ygg_dtype;
 
-typedef enum { YGG_OP_ATTENTION = 0, YGG_OP_EXPAND = 1, YGG_OP_ACCEPT = 2, YGG_OP_ATTACH = 3 } ygg_op;
+typedef enum {
+    YGG_OP_ATTENTION = 0, YGG_OP_EXPAND = 1, YGG_OP_ACCEPT = 2, YGG_OP_ATTACH = 3,
+    YGG_OP_ATTENTION_BLOCK8 = 4, YGG_OP_CONSTRAIN = 5
+} ygg_op;
 
 typedef struct {
     int32_t batch;         /* B >= 1 sequences, one tree each */
@@ -265,6 +278,116 @@ int32_t ygg_accept_and_compact(const ygg_shape *shape, int32_t n_layers,
                                void *k_cache, void *v_cache, int32_t *seq_lens,
                                int32_t *accept_len, int32_t *accept_path, int32_t *bonus_token,
                                void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * A K/V cache in 8 bits with one scale per block of YGG_KV_BLOCK tokens and kv head, for one layer (or, given to
+ * ygg_block8_append, for n_layers layers, one behind the other in each array).  nblk = ceil(kv_capacity / 64) blocks a sequence.
+ *
+ *   k_codes, v_codes [B,Hkv,nblk,64*Dh] E4M3 codes (as for ygg_tree_attention_fp8kv): a stored element is scale * value(code)
+ *   k_scale, v_scale [B,Hkv,nblk] fp32, at least 2^-100 and finite
+ *   k_tail,  v_tail  [B,128,Hkv,Dh] bf16: the row of token p is p % 128
+ *
+ * With L = seq_lens[b], tokens 0 .. 64*(L/64) - 1 are read from the blocks and the last L % 64 from the tail; nothing else of a
+ * cache is read.  A block is written once, when its last token arrives, from the bf16 rows of all its tokens.  The tail holds two
+ * blocks, so seq_lens[b] may be taken back to any token of the block before the open one that has not been overwritten since.
+ * Inside a block the codes lie in the order in which the matrix instructions of gfx950 take them, so that a block is streamed as
+ * it is stored: with token t (0..63) and dimension d, the code is at byte 1024*chunk + 16*lane + e,
+ *   K: chunk = 2*((t/32)*(Dh/64) + d/64) + d/16%2,  lane = 32*(d/32%2) + t%32,  e = d%16
+ *   V: chunk = 2*(d/32) + t/32,                     lane = 32*(t/4%2) + d%32,   e = 4*(t%32/8) + t%4
+ */
+#define YGG_KV_BLOCK 64
+typedef struct {
+    void *k_codes, *v_codes;   /* 16-byte aligned, as the tails */
+    float *k_scale, *v_scale;
+    void *k_tail, *v_tail;
+} ygg_block8_cache;
+
+/*
+ * Tree attention (see ygg_tree_attention) of one layer over such a cache; shape->kv_dtype == YGG_FP8_BLOCK, head_dim 64 or 128.
+ * A tree of one node (n_nodes 1, depth 0) is plain decoding.  The keys and values of cache and tree must be finite.
+ *   q, out [B,N,Hq,Dh] bf16;  k_tree, v_tree [B,N,Hkv,Dh] bf16;  lse [B,N,Hq] fp32 or NULL;  seq_lens, parent_idx int32
+ * q (bf16, 8 bits of significand) and the softmax weights enter the products as sums of two E4M3 values, that is with 8 bits and
+ * an exponent per row and tile; scores, softmax and accumulation are fp32.  Workspace: ygg_workspace_bytes(ATTENTION_BLOCK8).
+ */
+int32_t ygg_tree_attention_block8(const ygg_shape *shape, const void *q, const ygg_block8_cache *cache /* host struct */,
+                                  const int32_t *seq_lens, const void *k_tree, const void *v_tree,
+                                  const int32_t *parent_idx, void *out, float *lse,
+                                  void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Appends new tokens to such a cache, all layers in one launch: the K/V bookkeeping that ygg_accept_and_compact does for plain
+ * caches (call it with n_layers = 0 and hand its accept_path, accept_len and seq_lens to this), or a prompt's K/V.
+ *   k_new, v_new [n_layers,B,n_rows,Hkv,Dh] bf16: the tree's, or the prompt's, rows
+ *   rows         [B,max_new] int32: token k of the new ones is row rows[b][k]; NULL: row k.  Out-of-range rows count as zeros
+ *   n_new        [B] int32: new tokens of sequence b, 0 .. max_new (clamped to that)
+ *   seq_lens     [B] int32: the lengths AFTER the append (only read; clamped to kv_capacity); tokens seq_lens[b] - n_new[b] ..
+ *                seq_lens[b] - 1 are written
+ * Rows of the open block go to the tail as they are; a block that is completed is encoded: scale = max|x| / 448 over its 64
+ * tokens of one head (1 if all are zero, never below 2^-100), code = the E4M3 value nearest to x / scale, ties to even.
+ * Requires max_new <= n_rows unless rows is given.  Needs no workspace.
+ */
+int32_t ygg_block8_append(const ygg_shape *shape, int32_t n_layers, const void *k_new, const void *v_new, int32_t n_rows,
+                          const int32_t *rows, int32_t max_new, const int32_t *n_new, const int32_t *seq_lens,
+                          const ygg_block8_cache *cache /* host struct */, void *hip_stream);
+
+/*
+ * Rotary positions.  For pair j of the first rotary_dim dimensions of every head of token i of sequence b, at position p,
+ *     (x_j, x_j') <- scale * (x_j cos a - x_j' sin a,  x_j' cos a + x_j sin a),   a = p * frequencies[j]
+ * with (j, j') = (j, j + rotary_dim/2), or (2j, 2j+1) if interleaved; further dimensions are copied.  Angles are formed in fp64.
+ *   p            seq_lens[b] + depth of node i (parent_idx), or positions[b][i] if positions is given (then n_nodes is any number of
+ *                tokens per sequence, not a tree's, and seq_lens and parent_idx are not read)
+ *   q, q_out [B,N,Hq,Dh], k, k_out [B,N,Hkv,Dh]: fp32 for kv_dtype YGG_F32, else bf16.  One of the pairs may be NULL.  Tokens of
+ *                q and k are q_stride and k_stride elements apart (0: dense), so that parts of a fused projection can be given;
+ *                outputs are dense and may be the inputs where these are dense, else must not overlap them
+ *   frequencies  [rotary_dim/2] fp64 device, radians per position: scaled ones for long contexts are the caller's table
+ *   rotary_dim   a multiple of 16 up to head_dim;  scale: finite (1, or the factor that goes with a frequency scaling)
+ */
+int32_t ygg_tree_rotary(const ygg_shape *shape, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                        void *q_out, void *k_out, const double *frequencies, int32_t rotary_dim, int32_t interleaved,
+                        float scale, const int32_t *seq_lens, const int32_t *parent_idx, const int32_t *positions,
+                        void *hip_stream);
+
+/*
+ * Adds tokens to the counts that ygg_constrain_logits goes by.
+ *   tokens [B,n_tokens] int32;  rows [B,max_new] int32 or NULL: the k-th token added is tokens[b][rows[b][k]], or tokens[b][first+k]
+ *   n_new  [B] int32: tokens to add, 0 .. max_new (clamped to that);  prompt != 0: marks them as the prompt's instead of counting
+ *   counts [B,V] int32, in/out: bits 0-30 how often a token occurs in the confirmed reply, sign bit: it occurs in the prompt
+ * After ygg_accept_and_compact: tokens = the tree's token_ids, rows = accept_path, n_new = accept_len.  Tokens outside [0,V) and
+ * rows outside [0,n_tokens) are left out.  The caller zeroes counts when a sequence begins.
+ */
+int32_t ygg_count_tokens(const ygg_shape *shape, const int32_t *tokens, int32_t n_tokens, const int32_t *rows, int32_t first,
+                         int32_t max_new, const int32_t *n_new, int32_t prompt, int32_t *counts, void *hip_stream);
+
+/*
+ * Constrains the logits of every tree node and / or finds each row's first maximum.  With c = the token's count in `counts` plus its
+ * occurrences on the node's path (root .. node, token_ids), x = logit of node i of sequence b and token v, in fp32 and in this order:
+ *     if v occurs in counts[b] (reply or prompt) or on the path:  x <- x > 0 ? x / repetition[b] : x * repetition[b]
+ *     x <- x - frequency[b] * c;   if c > 0:  x <- x - presence[b];   x <- x + bias[b][v]
+ *     if mask_index[b][i] = m >= 0 and bit v%32 of masks[m][v/32] is 0:  x <- -inf
+ *     out[b,i,v] = x;   best[b,i] = argmax_v x (first maximum)
+ * `out` feeds ygg_equal_growth_expand / _attach and ygg_accept_and_compact, `best` the latter's target_tokens.
+ */
+typedef struct {
+    const int32_t *counts;      /* [B,V] device (ygg_count_tokens), or NULL: only the path counts */
+    const float *repetition;    /* [B] device, > 0, or NULL: 1 */
+    const float *presence;      /* [B] device or NULL: 0 */
+    const float *frequency;     /* [B] device or NULL: 0 */
+    const float *bias;          /* [B,V] device or NULL; -inf forbids a token */
+    int32_t bias_shared;        /* != 0: bias is [V], the same for all sequences */
+    int32_t n_masks;
+    const uint32_t *masks;      /* [n_masks, ceil(V/32)] device or NULL */
+    const int32_t *mask_index;  /* [B,N] device, required with masks; an index beyond n_masks - 1 counts as the last */
+} ygg_logit_rules;
+
+/*
+ *   logits     [B,N,V]: fp32 or bf16 (logits_dtype YGG_F32 / YGG_BF16), rows row_stride elements apart (0: V)
+ *   out        [B,N,V] fp32, or NULL; may be `logits` where those are dense and fp32
+ *   best       [B,N] int32, or NULL (then no workspace is needed); one of out and best must be given
+ * Workspace: ygg_workspace_bytes(CONSTRAIN).
+ */
+int32_t ygg_constrain_logits(const ygg_shape *shape, const void *logits, int32_t logits_dtype, int64_t row_stride,
+                             const int32_t *parent_idx, const int32_t *token_ids, const ygg_logit_rules *rules /* host struct */,
+                             float *out, int32_t *best, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
  * Debug validator for the data-dependent part of the contract above (the paper's runtime keeps the

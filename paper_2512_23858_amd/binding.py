@@ -9,14 +9,16 @@ from __future__ import annotations
 
 import ctypes
 import importlib
+import math
 import os
 from dataclasses import dataclass
 
 import torch
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
-OP_ATTENTION, OP_EXPAND, OP_ACCEPT, OP_ATTACH = 0, 1, 2, 3
-F32, BF16, FP8_E4M3 = 0, 1, 2
+OP_ATTENTION, OP_EXPAND, OP_ACCEPT, OP_ATTACH, OP_ATTENTION_BLOCK8, OP_CONSTRAIN = 0, 1, 2, 3, 4, 5
+F32, BF16, FP8_E4M3, FP8_BLOCK = 0, 1, 2, 3
+KV_BLOCK = 64      # tokens to a block of the 8-bit block cache
 
 
 class _CShape(ctypes.Structure):
@@ -48,6 +50,25 @@ class Shape:
         return _CShape(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim, self.depth, self.width,
                        self.n_nodes, self.vocab, self.kv_dtype, self.softmax_scale, self.kv_capacity,
                        self.max_seq_len)
+
+
+@dataclass
+class BlockCache:
+    """The tensors of an 8-bit block cache (ygg_block8_cache in include/ygg.h), of one layer or with a leading layer dimension:
+    codes [B,Hkv,nblk,64*Dh] uint8, scales [B,Hkv,nblk] fp32, tails [B,128,Hkv,Dh] bf16."""
+    k_codes: torch.Tensor
+    v_codes: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+    k_tail: torch.Tensor
+    v_tail: torch.Tensor
+
+    def tensors(self):
+        return self.k_codes, self.v_codes, self.k_scale, self.v_scale, self.k_tail, self.v_tail
+
+    def layer(self, i: int) -> "BlockCache":
+        """Views of one layer."""
+        return BlockCache(*(t[i] for t in self.tensors()))
 
 
 _lib = None
@@ -90,6 +111,12 @@ def load_library() -> ctypes.CDLL:
         lib.ygg_debug_validate.argtypes = [shp] + [vp] * 4 + [i32, vp, vp]
         lib.ygg_accept_and_compact.restype = i32
         lib.ygg_accept_and_compact.argtypes = [shp, i32] + [vp] * 12 + [vp, sz, vp]
+        for name, args in (("ygg_tree_attention_block8", [shp] + [vp] * 8 + [vp, sz, vp]),
+                           ("ygg_block8_append", [shp, i32, vp, vp, i32, vp, i32, vp, vp, vp, vp]),
+                           ("ygg_tree_rotary", [shp, vp, ctypes.c_int64, vp, ctypes.c_int64] + [vp] * 3 + [i32, i32, ctypes.c_float] + [vp] * 4),
+                           ("ygg_count_tokens", [shp, vp, i32, vp, i32, i32, vp, i32, vp, vp]),
+                           ("ygg_constrain_logits", [shp, vp, i32, ctypes.c_int64] + [vp] * 5 + [vp, sz, vp])):
+            getattr(lib, name).restype, getattr(lib, name).argtypes = i32, args
         lib.ygg_init.restype = i32
         lib.ygg_init.argtypes = []
         lib.ygg_debug_set_attention_plan.restype = i32
@@ -131,6 +158,31 @@ def new_workspace(shape: Shape, op: int, n_layers: int = 0, device="cuda:0"):
     if n == 0:
         raise ValueError("invalid shape for a workspace")
     return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def new_block_cache(shape: Shape, n_layers: int = 1, device="cuda:0") -> BlockCache:
+    """Allocates an empty 8-bit block cache of n_layers layers through torch (zeros)."""
+    if workspace_bytes(shape, OP_ATTENTION_BLOCK8) == 0:
+        raise ValueError("invalid shape for a block cache")
+    B, Hkv, Dh, nblk = shape.batch, shape.n_kv_heads, shape.head_dim, -(-shape.kv_capacity // KV_BLOCK)
+    codes, scales, tails = (n_layers, B, Hkv, nblk, KV_BLOCK * Dh), (n_layers, B, Hkv, nblk), (n_layers, B, 2 * KV_BLOCK, Hkv, Dh)
+    return BlockCache(*(torch.zeros(codes, dtype=torch.uint8, device=device) for _ in range(2)),
+                      *(torch.ones(scales, dtype=torch.float32, device=device) for _ in range(2)),
+                      *(torch.zeros(tails, dtype=torch.bfloat16, device=device) for _ in range(2)))
+
+
+def rotary_frequencies(rotary_dim: int, base: float = 10000.0, factor: float = 1.0, original_len: int = 0,
+                       low_turns: float = 1.0, high_turns: float = 4.0) -> torch.Tensor:
+    """Frequency table [rotary_dim/2] of tree_rotary on the host, fp64: base^(-2j/rotary_dim) radians per position.
+    factor > 1 stretches positions for long contexts: all frequencies alike where original_len is 0; else those that make at most
+    low_turns turns over original_len positions in full, those that make high_turns or more not at all, with a ramp between."""
+    if rotary_dim < 2 or rotary_dim % 2 or not base > 0 or not factor > 0 or original_len < 0 or not high_turns > low_turns:
+        raise ValueError("rotary_dim must be even, base and factor positive, original_len not negative, high_turns above low_turns")
+    f = float(base) ** (-torch.arange(rotary_dim // 2, dtype=torch.float64) * 2 / rotary_dim)
+    keep = torch.zeros_like(f)
+    if original_len:
+        keep = ((original_len * f / (2 * math.pi) - low_turns) / (high_turns - low_turns)).clamp(0, 1)
+    return f * keep + f / factor * (1 - keep)
 
 
 def _dev(t, dtype=None, name="tensor"):
@@ -274,6 +326,100 @@ def accept_and_compact(shape: Shape, n_layers: int, parent_idx, token_ids, k_tre
                      (accept_len, i32, "accept_len"), (accept_path, i32, "accept_path"), (bonus_token, i32, "bonus_token"),
                      (workspace, None, "workspace"))
         _check(rc, "ygg_accept_and_compact")
+
+
+def _explain_rows(shape, rows, *checks):
+    """_explain for calls with tensors whose rows may be strided: rows = (tensor, wanted dtype or None, name)."""
+    for t, dtype, name in rows:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a GPU tensor")
+        if dtype is not None and t.dtype != dtype:
+            raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+        if t.dim() < 3:
+            raise ValueError(f"{name} must have batch and token dimensions and dense ones behind them")
+    for t, dtype, name in checks:
+        _dev(t, dtype, name)
+    for t, _, name in rows:
+        if t is not None and not t.is_contiguous():
+            raise ValueError(f"{name}: rows must be dense and lie evenly over batch and tokens")
+    _explain(shape)
+
+
+def _cache_checks(cache: BlockCache):
+    want = (torch.uint8, torch.uint8, torch.float32, torch.float32, torch.bfloat16, torch.bfloat16)
+    return list(zip(cache.tensors(), want, ("k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail")))
+
+
+def tree_attention_block8(shape: Shape, q, cache: BlockCache, seq_lens, k_tree, v_tree, parent_idx, out, lse=None, workspace=None):
+    """ygg_tree_attention_block8: tree attention of one layer over an 8-bit block cache (shape.kv_dtype FP8_BLOCK)."""
+    rc = (_native or _calls()).tree_attention_block8(shape, q, cache.k_codes, cache.v_codes, cache.k_scale, cache.v_scale, cache.k_tail,
+                                                     cache.v_tail, seq_lens, k_tree, v_tree, parent_idx, out, lse, workspace)
+    if rc:
+        if rc < 0:
+            bf, i32 = torch.bfloat16, torch.int32
+            _explain(shape, (q, bf, "q"), *_cache_checks(cache), (seq_lens, i32, "seq_lens"), (k_tree, bf, "k_tree"),
+                     (v_tree, bf, "v_tree"), (parent_idx, i32, "parent_idx"), (out, bf, "out"), (lse, torch.float32, "lse"),
+                     (workspace, None, "workspace"))
+        _check(rc, "ygg_tree_attention_block8")
+    return out
+
+
+def block8_append(shape: Shape, n_layers: int, k_new, v_new, cache: BlockCache, seq_lens, n_new, rows=None):
+    """ygg_block8_append: tokens seq_lens - n_new .. seq_lens - 1 of every layer, from rows of k_new and v_new
+    [n_layers,B,n_rows,Hkv,Dh]; rows [B,max_new] picks them (an accept_path), else they are the first n_new."""
+    rc = (_native or _calls()).block8_append(shape, n_layers, k_new, v_new, rows, n_new, seq_lens, cache.k_codes, cache.v_codes,
+                                             cache.k_scale, cache.v_scale, cache.k_tail, cache.v_tail)
+    if rc:
+        if rc < 0:
+            bf, i32 = torch.bfloat16, torch.int32
+            _explain(shape, (k_new, bf, "k_new"), (v_new, bf, "v_new"), (rows, i32, "rows"), (n_new, i32, "n_new"),
+                     (seq_lens, i32, "seq_lens"), *_cache_checks(cache))
+        _check(rc, "ygg_block8_append")
+
+
+def tree_rotary(shape: Shape, q, k, q_out, k_out, frequencies, seq_lens=None, parent_idx=None, positions=None, interleaved: bool = False,
+                scale: float = 1.0):
+    """ygg_tree_rotary: rotates 2 * len(frequencies) dimensions of every head of q [B,N,Hq,Dh] and k [B,N,Hkv,Dh] (either may be None
+    with its output; tokens may be strided) at seq_lens + depth, or at positions [B,N].  frequencies: fp64 on the GPU."""
+    rc = (_native or _calls()).tree_rotary(shape, q, k, q_out, k_out, frequencies, seq_lens, parent_idx, positions,
+                                           True if interleaved else False, scale)
+    if rc:
+        if rc < 0:
+            dt, i32 = torch.float32 if shape.kv_dtype == F32 else torch.bfloat16, torch.int32
+            _explain_rows(shape, ((q, dt, "q"), (k, dt, "k")), (q_out, dt, "q_out"), (k_out, dt, "k_out"),
+                          (frequencies, torch.float64, "frequencies"), (seq_lens, i32, "seq_lens"), (parent_idx, i32, "parent_idx"),
+                          (positions, i32, "positions"))
+        _check(rc, "ygg_tree_rotary")
+
+
+def count_tokens(shape: Shape, tokens, n_new, counts, rows=None, first: int = 0, prompt: bool = False):
+    """ygg_count_tokens: adds n_new[b] tokens of tokens [B,T] (from `first` on, or those that rows [B,max_new] names) to counts [B,V]."""
+    rc = (_native or _calls()).count_tokens(shape, tokens, n_new, counts, rows, first, True if prompt else False)
+    if rc:
+        if rc < 0:
+            i32 = torch.int32
+            _explain(shape, (tokens, i32, "tokens"), (n_new, i32, "n_new"), (counts, i32, "counts"), (rows, i32, "rows"))
+        _check(rc, "ygg_count_tokens")
+
+
+def constrain_logits(shape: Shape, logits, parent_idx, token_ids, out=None, best=None, counts=None, repetition=None, presence=None,
+                     frequency=None, bias=None, masks=None, mask_index=None, workspace=None):
+    """ygg_constrain_logits: penalties, bias ([V] or [B,V]) and masks ([M, ceil(V/32)] int32 bit words) on logits [B,N,V] (fp32 or
+    bf16, rows may be strided) into `out` (fp32) and / or the first maximum of each row into `best`."""
+    rc = (_native or _calls()).constrain_logits(shape, logits, parent_idx, token_ids, out, best, counts, repetition, presence, frequency,
+                                                bias, masks, mask_index, workspace)
+    if rc:
+        if rc < 0:
+            f32, i32 = torch.float32, torch.int32
+            if logits is not None and logits.dtype not in (f32, torch.bfloat16):
+                raise TypeError(f"logits: expected {f32} or {torch.bfloat16}, got {logits.dtype}")
+            _explain_rows(shape, ((logits, None, "logits"),), (parent_idx, i32, "parent_idx"), (token_ids, i32, "token_ids"),
+                          (out, f32, "out"), (best, i32, "best"), (counts, i32, "counts"), (repetition, f32, "repetition"),
+                          (presence, f32, "presence"), (frequency, f32, "frequency"), (bias, f32, "bias"), (masks, i32, "masks"),
+                          (mask_index, i32, "mask_index"), (workspace, None, "workspace"))
+        _check(rc, "ygg_constrain_logits")
 
 
 def attention_plan(shape: Shape) -> dict:

@@ -1,0 +1,184 @@
+// Penalties, biases and grammar masks on logits, with each row's first maximum.
+//
+//   constrain_kernel  one workgroup per (tree node, chunk of the vocabulary).  The node's path is walked in LDS and its tokens are
+//                     counted into a table of the chunk; then the chunk streams through once, four logits to a thread and step, each
+//                     with its confirmed count, path count, bias and mask bit.  The arithmetic is fp32, one rounding per step as
+//                     the definition has it (no fused multiply-add), so that equal inputs give equal ties.
+//   best_kernel       the chunks' maxima of a row, first maximum.
+// Bound by the stream of logits in and out; counts and biases of a sequence are read by all of its nodes and stay in L2.
+#include "ygg_internal.h"
+#include "ygg_device.h"
+
+#include <algorithm>
+
+namespace ygg {
+namespace {
+
+constexpr int kChunk = 4096;
+
+struct Best {
+    float val;
+    int32_t idx;
+};
+__device__ __forceinline__ void take_first(float& v, int& i, float v2, int i2) {
+    if (v2 > v || (v2 == v && i2 < i)) { v = v2; i = i2; }
+}
+
+// Rows start at any element, so vectors are only as aligned as their elements.
+struct __attribute__((packed, aligned(4))) F4 { float x[4]; };
+struct __attribute__((packed, aligned(4))) I4 { int32_t x[4]; };
+struct __attribute__((packed, aligned(2))) H4 { uint16_t x[4]; };
+
+template <typename T>
+__device__ __forceinline__ float logit_of(T v) {
+    if constexpr (sizeof(T) == 4) return v;
+    else return __uint_as_float((uint32_t)v << 16);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void constrain_kernel(ConstrainArgs a) {
+    __shared__ int32_t parent_s[kMaxNodes];
+    __shared__ int32_t token_s[kMaxNodes];
+    __shared__ __align__(8) uint16_t times_s[kChunk];   // occurrences on the path, by token of the chunk
+    __shared__ Best best_s[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t row = blockIdx.x;   // b * N + i
+    const int b = (int)(row / a.N), i = (int)(row - (int64_t)b * a.N);
+    const int c0 = blockIdx.y * kChunk, c1 = min(a.V, c0 + kChunk);
+
+    for (int n = tid; n <= i; n += 256) {
+        parent_s[n] = a.parent_idx[(int64_t)b * a.N + n];
+        token_s[n] = a.token_ids[(int64_t)b * a.N + n];
+    }
+    for (int n = tid; n < kChunk / 8; n += 256) reinterpret_cast<uint4*>(times_s)[n] = make_uint4(0, 0, 0, 0);
+    const float repetition = a.repetition ? a.repetition[b] : 1.f;
+    const float presence = a.presence ? a.presence[b] : 0.f, frequency = a.frequency ? a.frequency[b] : 0.f;
+    const uint32_t* mask = nullptr;
+    if (a.masks) {
+        const int m = a.mask_index[row];
+        if (m >= 0) mask = a.masks + (int64_t)min(m, a.n_masks - 1) * ((a.V + 31) / 32);
+    }
+    __syncthreads();
+    if (tid == 0)
+        for (int n = i;;) {   // a parent that is no earlier node ends the walk
+            const int t = token_s[n];
+            if (t >= c0 && t < c1) ++times_s[t - c0];
+            const int p = parent_s[n];
+            if (p < 0 || p >= n) break;
+            n = p;
+        }
+    __syncthreads();
+
+    const T* x = static_cast<const T*>(a.logits) + row * a.row_stride;
+    const int32_t* counts = a.counts ? a.counts + (int64_t)b * a.V : nullptr;
+    const float* bias = a.bias ? a.bias + (a.bias_shared ? 0 : (int64_t)b * a.V) : nullptr;
+    float* out = a.out ? a.out + row * a.V : nullptr;
+    float bv = -INFINITY;
+    int bi = 0x7fffffff;
+    auto constrained = [&](float v, int32_t confirmed, uint32_t times, float add, bool allowed) {
+        const uint32_t c = ((uint32_t)confirmed & 0x7fffffffu) + times;
+        if (confirmed != 0 || times) v = v > 0.f ? __fdiv_rn(v, repetition) : __fmul_rn(v, repetition);
+        v = __fsub_rn(v, __fmul_rn(frequency, (float)c));
+        v = __fsub_rn(v, c ? presence : 0.f);
+        if (bias) v = __fadd_rn(v, add);
+        return allowed ? v : -INFINITY;
+    };
+    for (int j = c0 + 4 * tid; j < c1; j += 1024) {
+        if (j + 4 <= c1) {
+            float v[4];
+            if constexpr (sizeof(T) == 4) {
+                const F4 q = *reinterpret_cast<const F4*>(x + j);
+                for (int e = 0; e < 4; ++e) v[e] = q.x[e];
+            } else {
+                const H4 q = *reinterpret_cast<const H4*>(x + j);
+                for (int e = 0; e < 4; ++e) v[e] = logit_of(q.x[e]);
+            }
+            I4 n = {};
+            F4 add = {};
+            if (counts) n = *reinterpret_cast<const I4*>(counts + j);
+            if (bias) add = *reinterpret_cast<const F4*>(bias + j);
+            const uint32_t bits = mask ? mask[j >> 5] >> (j & 31) : 0xfu;
+            const uint2 times = *reinterpret_cast<const uint2*>(times_s + (j - c0));
+            F4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t t = ((e < 2 ? times.x : times.y) >> (16 * (e & 1))) & 0xffffu;
+                y.x[e] = constrained(v[e], n.x[e], t, add.x[e], (bits >> e) & 1u);
+                if (y.x[e] > bv || bi == 0x7fffffff) { bv = y.x[e]; bi = j + e; }
+            }
+            if (out) *reinterpret_cast<F4*>(out + j) = y;
+        } else {
+            for (int e = j; e < c1; ++e) {
+                const float y = constrained(logit_of(x[e]), counts ? counts[e] : 0, times_s[e - c0], bias ? bias[e] : 0.f,
+                                            !mask || ((mask[e >> 5] >> (e & 31)) & 1u));
+                if (y > bv || bi == 0x7fffffff) { bv = y; bi = e; }
+                if (out) out[e] = y;
+            }
+        }
+    }
+    if (!a.best) return;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) take_first(bv, bi, __shfl_xor(bv, o), __shfl_xor(bi, o));
+    if (lane == 0) best_s[wave] = {bv, bi};
+    __syncthreads();
+    if (tid == 0) {
+#pragma unroll
+        for (int w = 1; w < 4; ++w) take_first(bv, bi, best_s[w].val, best_s[w].idx);
+        if (gridDim.y == 1) a.best[row] = bi;
+        else static_cast<Best*>(a.part)[row * gridDim.y + blockIdx.y] = {bv, bi};
+    }
+}
+
+__global__ __launch_bounds__(256) void best_kernel(ConstrainArgs a, int64_t rows, int chunks) {
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (row >= rows) return;
+    const Best* p = static_cast<const Best*>(a.part) + row * chunks;
+    float bv = -INFINITY;
+    int bi = 0x7fffffff;
+    for (int c = lane; c < chunks; c += 64) take_first(bv, bi, p[c].val, p[c].idx);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) take_first(bv, bi, __shfl_xor(bv, o), __shfl_xor(bi, o));
+    if (lane == 0) a.best[row] = bi;
+}
+
+__global__ __launch_bounds__(256) void count_kernel(CountArgs a) {
+    const int b = blockIdx.y;
+    const int n = min(a.n_new[b], a.max_new);
+    for (int k = blockIdx.x * 256 + threadIdx.x; k < n; k += gridDim.x * 256) {
+        const int64_t r = a.rows ? (int64_t)a.rows[(int64_t)b * a.max_new + k] : (int64_t)a.first + k;
+        if (r < 0 || r >= a.n_tokens) continue;
+        const int t = a.tokens[(int64_t)b * a.n_tokens + r];
+        if (t < 0 || t >= a.V) continue;
+        int32_t* c = a.counts + (int64_t)b * a.V + t;
+        if (a.prompt) atomicOr(c, (int32_t)0x80000000);
+        else atomicAdd(c, 1);
+    }
+}
+
+}  // namespace
+
+size_t constrain_scratch_bytes(const ygg_shape& s) {
+    const int64_t rows = (int64_t)s.batch * s.n_nodes, chunks = ((int64_t)s.vocab + kChunk - 1) / kChunk;
+    return ((size_t)(rows * chunks) * sizeof(Best) + 255) / 256 * 256;
+}
+
+hipError_t launch_constrain(const ConstrainArgs& a, bool f32, hipStream_t st) {
+    const int64_t rows = (int64_t)a.B * a.N;
+    const int chunks = (a.V + kChunk - 1) / kChunk;
+    const dim3 grid((unsigned)rows, (unsigned)chunks);
+    if (f32) hipLaunchKernelGGL((constrain_kernel<float>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((constrain_kernel<uint16_t>), grid, dim3(256), 0, st, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !a.best || chunks == 1) return e;
+    hipLaunchKernelGGL(best_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a, rows, chunks);
+    return hipGetLastError();
+}
+
+hipError_t launch_count(const CountArgs& a, hipStream_t st) {
+    const unsigned groups = (unsigned)std::clamp((a.max_new + 255) / 256, 1, 64);
+    hipLaunchKernelGGL(count_kernel, dim3(groups, (unsigned)a.B), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace ygg

@@ -83,6 +83,30 @@ struct Args {
         bytes = p ? THPVariable_Unpack(a[i]).nbytes() : 0;
         return p;
     }
+    // A tensor [B, N, ..] whose trailing dimensions are dense and whose B * N rows lie evenly: the row stride in elements
+    void* rows(int i, at::ScalarType want, int64_t& stride, bool any = false) {
+        PyObject* o = a[i];
+        stride = 0;
+        if (o == Py_None) return nullptr;
+        if (!THPVariable_Check(o)) { ok = false; return nullptr; }
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.is_cuda() || t.dim() < 3 || (!any && t.scalar_type() != want)) { ok = false; return nullptr; }
+        int64_t inner = 1;
+        for (int64_t d = t.dim() - 1; d >= 2; --d) {
+            if (t.size(d) > 1 && t.stride(d) != inner) { ok = false; return nullptr; }
+            inner *= t.size(d);
+        }
+        const int64_t B = t.size(0), N = t.size(1);
+        stride = N > 1 ? t.stride(1) : B > 1 ? t.stride(0) : inner;
+        if (B > 1 && N > 1 && t.stride(0) != N * stride) { ok = false; return nullptr; }
+        return t.data_ptr();
+    }
+    int32_t size(int i, int64_t d) {   // of a tensor that passed its check, else 0
+        if (!ok || a[i] == Py_None) return 0;
+        const at::Tensor& t = THPVariable_Unpack(a[i]);
+        if (d >= t.dim() || t.size(d) > INT32_MAX) { ok = false; return 0; }
+        return (int32_t)t.size(d);
+    }
     bool number(int i, int32_t& out) {
         const int64_t v = PyLong_AsLongLong(a[i]);
         if ((v == -1 && PyErr_Occurred()) || v < INT32_MIN || v > INT32_MAX) { PyErr_Clear(); return ok = false; }
@@ -229,6 +253,107 @@ PyObject* accept_and_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// The six tensors of a block cache, from argument i on
+ygg_block8_cache block_cache(Args& t, int i) {
+    ygg_block8_cache c{};
+    c.k_codes = t.ptr(i, at::kByte); c.v_codes = t.ptr(i + 1, at::kByte);
+    c.k_scale = t.floats(i + 2); c.v_scale = t.floats(i + 3);
+    c.k_tail = t.ptr(i + 4, at::kBFloat16); c.v_tail = t.ptr(i + 5, at::kBFloat16);
+    return c;
+}
+
+// (shape, q, k_codes, v_codes, k_scale, v_scale, k_tail, v_tail, seq_lens, k_tree, v_tree, parent_idx, out, lse, workspace)
+PyObject* tree_attention_block8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!arity(n, 15)) return nullptr;
+    ygg_shape s{};
+    Args t{a};
+    t.ok = read_shape(a[0], s);
+    const ygg_block8_cache c = block_cache(t, 2);
+    void *q = t.ptr(1, at::kBFloat16), *kt = t.ptr(9, at::kBFloat16), *vt = t.ptr(10, at::kBFloat16), *out = t.ptr(12, at::kBFloat16);
+    int32_t *lens = t.ints(8), *parent = t.ints(11);
+    float* lse = t.floats(13);
+    size_t wn;
+    void* ws = t.scratch(14, wn);
+    return finish(t.ok, [&](void* st) { return ygg_tree_attention_block8(&s, q, &c, lens, kt, vt, parent, out, lse, ws, wn, st); });
+}
+
+// (shape, n_layers, k_new, v_new, rows, n_new, seq_lens, k_codes, v_codes, k_scale, v_scale, k_tail, v_tail)
+PyObject* block8_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!arity(n, 13)) return nullptr;
+    ygg_shape s{};
+    Args t{a};
+    t.ok = read_shape(a[0], s);
+    int32_t layers = 0;
+    t.number(1, layers);
+    void *k = t.ptr(2, at::kBFloat16), *v = t.ptr(3, at::kBFloat16);
+    int32_t *rows = t.ints(4), *n_new = t.ints(5), *lens = t.ints(6);
+    const ygg_block8_cache c = block_cache(t, 7);
+    const int32_t n_rows = t.size(2, 2), most = rows ? t.size(4, 1) : n_rows;
+    return finish(t.ok, [&](void* st) { return ygg_block8_append(&s, layers, k, v, n_rows, rows, most, n_new, lens, &c, st); });
+}
+
+// (shape, q, k, q_out, k_out, frequencies, seq_lens, parent_idx, positions, interleaved, scale)
+PyObject* tree_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!arity(n, 11)) return nullptr;
+    ygg_shape s{};
+    Args t{a};
+    t.ok = read_shape(a[0], s);
+    const at::ScalarType dt = s.kv_dtype == YGG_F32 ? at::kFloat : at::kBFloat16;
+    int64_t qs, ks;
+    void *q = t.rows(1, dt, qs), *k = t.rows(2, dt, ks), *qo = t.ptr(3, dt), *ko = t.ptr(4, dt);
+    const double* f = t.typed<double>(5, at::kDouble);
+    const int32_t pairs = t.size(5, 0);
+    int32_t *lens = t.ints(6), *parent = t.ints(7), *positions = t.ints(8);
+    const bool interleaved = a[9] == Py_True;
+    const double scale = PyFloat_AsDouble(a[10]);
+    if (PyErr_Occurred()) { PyErr_Clear(); t.ok = false; }
+    return finish(t.ok && pairs <= 1024, [&](void* st) {
+        return ygg_tree_rotary(&s, q, qs, k, ks, qo, ko, f, 2 * pairs, interleaved, (float)scale, lens, parent, positions, st);
+    });
+}
+
+// (shape, tokens, n_new, counts, rows, first, prompt)
+PyObject* count_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!arity(n, 7)) return nullptr;
+    ygg_shape s{};
+    Args t{a};
+    t.ok = read_shape(a[0], s);
+    int32_t *tokens = t.ints(1), *n_new = t.ints(2), *counts = t.ints(3), *rows = t.ints(4);
+    int32_t first = 0;
+    t.number(5, first);
+    const int32_t n_tokens = t.size(1, 1), most = rows ? t.size(4, 1) : n_tokens;
+    const bool prompt = a[6] == Py_True;
+    return finish(t.ok, [&](void* st) { return ygg_count_tokens(&s, tokens, n_tokens, rows, first, most, n_new, prompt, counts, st); });
+}
+
+// (shape, logits, parent_idx, token_ids, out, best, counts, repetition, presence, frequency, bias, masks, mask_index, workspace)
+PyObject* constrain_logits(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!arity(n, 14)) return nullptr;
+    ygg_shape s{};
+    Args t{a};
+    t.ok = read_shape(a[0], s);
+    int64_t stride;
+    void* x = t.rows(1, at::kFloat, stride, true);
+    int32_t dt = -1;
+    if (t.ok && x) {
+        const at::ScalarType type = THPVariable_Unpack(a[1]).scalar_type();
+        dt = type == at::kFloat ? YGG_F32 : type == at::kBFloat16 ? YGG_BF16 : -1;
+        t.ok = dt >= 0;
+    }
+    int32_t *parent = t.ints(2), *token = t.ints(3), *best = t.ints(5);
+    float* out = t.floats(4);
+    ygg_logit_rules r{};
+    r.counts = t.ints(6);
+    r.repetition = t.floats(7); r.presence = t.floats(8); r.frequency = t.floats(9); r.bias = t.floats(10);
+    r.bias_shared = r.bias && t.ok && THPVariable_Unpack(a[10]).dim() == 1;
+    r.masks = reinterpret_cast<const uint32_t*>(t.ints(11));
+    r.n_masks = t.size(11, 0);
+    r.mask_index = t.ints(12);
+    size_t wn;
+    void* ws = t.scratch(13, wn);
+    return finish(t.ok, [&](void* st) { return ygg_constrain_logits(&s, x, dt, stride, parent, token, &r, out, best, ws, wn, st); });
+}
+
 // torch reports its errors (no device, a tensor without storage) as C++ exceptions
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n) {
@@ -243,7 +368,9 @@ PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n) {
 #define YGG_CALL(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<name>)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {
     YGG_CALL(tree_attention), YGG_CALL(tree_attention_fp8kv), YGG_CALL(equal_growth_expand), YGG_CALL(equal_growth_expand_static),
-    YGG_CALL(equal_growth_attach), YGG_CALL(prune_for_verification), YGG_CALL(accept_and_compact), {nullptr, nullptr, 0, nullptr}};
+    YGG_CALL(equal_growth_attach), YGG_CALL(prune_for_verification), YGG_CALL(accept_and_compact),
+    YGG_CALL(tree_attention_block8), YGG_CALL(block8_append), YGG_CALL(tree_rotary), YGG_CALL(count_tokens),
+    YGG_CALL(constrain_logits), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_calls", "native argument marshalling of the launching calls", -1, kMethods,
                        nullptr, nullptr, nullptr, nullptr};

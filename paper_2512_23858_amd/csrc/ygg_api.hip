@@ -58,6 +58,22 @@ int32_t check_shape(const ygg_shape* s, bool need_kv, bool need_vocab) {
     return YGG_OK;
 }
 
+// Shapes of the calls on the 8-bit block cache.
+int32_t check_block8(const ygg_shape* s) {
+    if (int32_t rc = check_shape(s, false, false)) return rc;
+    if (s->kv_dtype != YGG_FP8_BLOCK || (s->head_dim != 64 && s->head_dim != 128)) return YGG_ERR_UNSUPPORTED;
+    if (!(s->softmax_scale > 0.f) || !std::isfinite(s->softmax_scale)) return YGG_ERR_SHAPE;
+    return YGG_OK;
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+int32_t check_cache(const ygg_block8_cache* c) {
+    if (!c || !c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale || !c->k_tail || !c->v_tail) return YGG_ERR_NULL;
+    if (!aligned16(c->k_codes) || !aligned16(c->v_codes) || !aligned16(c->k_tail) || !aligned16(c->v_tail)) return YGG_ERR_UNSUPPORTED;
+    return YGG_OK;
+}
+
 int32_t check_workspace(const void* ws, size_t have, size_t need) {
     if (need == 0) return YGG_OK;
     if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0 || have < need) return YGG_ERR_WORKSPACE;
@@ -256,6 +272,24 @@ static size_t attention_scratch_bytes(const ygg_shape& s) {
     return part_o_bytes(s, p.use_mfma, most) + part_rec_bytes(s, most) + p.seq_splits_bytes;
 }
 
+// Workgroup shape and runs of the attention over the block cache.
+Block8Plan plan_block8(const ygg_shape& s) {
+    Block8Plan p{};
+    const int64_t R = (int64_t)s.n_nodes * (s.n_q_heads / s.n_kv_heads);
+    p.row_blocks = R <= 32 ? 1 : R <= 64 ? 2 : R <= 128 ? 4 : 8;
+    p.row_tiles = (int32_t)((R + p.row_blocks * 32 - 1) / (p.row_blocks * 32));
+    const int64_t per_stream = (int64_t)s.n_kv_heads * p.row_tiles;
+    const int64_t at_once = 256 / per_stream;                      // one workgroup to a compute unit
+    const int64_t tiles = (int64_t)s.batch * (s.max_seq_len / YGG_KV_BLOCK);
+    int64_t runs = std::max(at_once - s.batch, at_once / 2);
+    runs = std::min(runs, tiles);
+    p.runs = (int32_t)std::clamp(runs, (int64_t)1, (int64_t)63);   // the merge takes 64 splits, one is the sequence's own keys
+    p.part_o_bytes = part_o_bytes(s, true, p.runs + 1);
+    p.part_rec_bytes = part_rec_bytes(s, p.runs + 1);
+    p.seq_splits_bytes = align256((size_t)s.batch * sizeof(int32_t));
+    return p;
+}
+
 // Raises the shared-memory limits of the current device's kernels once; later calls cost one atomic load.
 int32_t ensure_device_ready() {
     int dev = 0;
@@ -263,7 +297,8 @@ int32_t ensure_device_ready() {
     if (g_device_ready[dev].load(std::memory_order_acquire)) return YGG_OK;
     std::lock_guard<std::mutex> lock(g_init_mutex);
     if (g_device_ready[dev].load(std::memory_order_relaxed)) return YGG_OK;
-    if (raise_limits_attn_mfma() != hipSuccess || raise_limits_expand() != hipSuccess) return YGG_ERR_LAUNCH;
+    if (raise_limits_attn_mfma() != hipSuccess || raise_limits_expand() != hipSuccess || raise_limits_attn_block8() != hipSuccess)
+        return YGG_ERR_LAUNCH;
     void* sp = nullptr;
     if (hipGetSymbolAddress(&sp, HIP_SYMBOL(scratch)) != hipSuccess || !sp) return YGG_ERR_LAUNCH;
     g_scratch_ptr[dev] = static_cast<unsigned char*>(sp);
@@ -331,6 +366,15 @@ size_t ygg_workspace_bytes(const ygg_shape* s, int32_t op, int32_t n_layers) {
         case YGG_OP_ACCEPT: {
             if (check_shape(s, false, true) != YGG_OK) return 0;
             return accept_scratch_bytes(*s);
+        }
+        case YGG_OP_ATTENTION_BLOCK8: {
+            if (check_block8(s) != YGG_OK) return 0;
+            const Block8Plan p = plan_block8(*s);
+            return p.part_o_bytes + p.part_rec_bytes + p.seq_splits_bytes;
+        }
+        case YGG_OP_CONSTRAIN: {
+            if (check_shape(s, false, true) != YGG_OK) return 0;
+            return constrain_scratch_bytes(*s);
         }
         default: return 0;
     }
@@ -540,6 +584,126 @@ int32_t ygg_accept_and_compact(const ygg_shape* s, int32_t n_layers, const float
     a.n_layers = n_layers; a.chunk = p.chunk; a.nchunk = p.nchunk; a.max_seq_len = s->max_seq_len;
     a.elem_bytes = s->kv_dtype == YGG_F32 ? 4 : s->kv_dtype == YGG_BF16 ? 2 : 1; a.cap = s->kv_capacity;
     return launch_accept(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? YGG_OK : YGG_ERR_LAUNCH;
+}
+
+int32_t ygg_tree_attention_block8(const ygg_shape* s, const void* q, const ygg_block8_cache* cache, const int32_t* seq_lens,
+                                  const void* k_tree, const void* v_tree, const int32_t* parent_idx, void* out, float* lse,
+                                  void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (int32_t rc = check_block8(s)) return rc;
+    if (int32_t rc = check_cache(cache)) return rc;
+    if (!q || !seq_lens || !k_tree || !v_tree || !parent_idx || !out) return YGG_ERR_NULL;
+    if (!aligned16(q) || !aligned16(k_tree) || !aligned16(v_tree) || !aligned16(out)) return YGG_ERR_UNSUPPORTED;
+    const int64_t rows = (int64_t)s->batch * s->n_nodes * s->n_q_heads;
+    const Block8Plan p = plan_block8(*s);
+    // the kernels count query rows, and workgroups, with 31 bits
+    if (rows > 0x7fffffffLL || ((int64_t)s->batch + p.runs + 8) * s->n_kv_heads * p.row_tiles > 0x7fffffffLL) return YGG_ERR_UNSUPPORTED;
+    if (int32_t rc = check_workspace(workspace, workspace_bytes, p.part_o_bytes + p.part_rec_bytes + p.seq_splits_bytes)) return rc;
+    if (int32_t rc = ensure_device_ready()) return rc;
+
+    Block8Args a{};
+    a.q = q; a.k_codes = cache->k_codes; a.v_codes = cache->v_codes; a.k_scale = cache->k_scale; a.v_scale = cache->v_scale;
+    a.k_tail = cache->k_tail; a.v_tail = cache->v_tail; a.k_tree = k_tree; a.v_tree = v_tree;
+    a.seq_lens = seq_lens; a.parent_idx = parent_idx;
+    a.part_o = workspace;
+    a.part_rec = reinterpret_cast<float3*>(static_cast<char*>(workspace) + p.part_o_bytes);
+    a.seq_splits = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + p.part_o_bytes + p.part_rec_bytes);
+    a.nblk = (s->kv_capacity + YGG_KV_BLOCK - 1) / YGG_KV_BLOCK;
+    a.rows_total = rows;
+    a.B = s->batch; a.N = s->n_nodes; a.Hq = s->n_q_heads; a.Hkv = s->n_kv_heads; a.G = a.Hq / a.Hkv; a.R = a.N * a.G;
+    a.row_tiles = p.row_tiles; a.runs = p.runs; a.max_seq_len = s->max_seq_len; a.scale = s->softmax_scale;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (launch_attn_block8(a, p, s->head_dim, st) != hipSuccess) return YGG_ERR_LAUNCH;
+
+    AttnArgs m{};      // the merge of the splits, shared with the other matrix-core kernels
+    m.part_o = a.part_o; m.part_rec = a.part_rec; m.seq_splits = a.seq_splits; m.out = out; m.lse = lse;
+    m.B = a.B; m.N = a.N; m.Hq = a.Hq; m.Hkv = a.Hkv; m.Dh = s->head_dim; m.nsplit = p.runs + 1; m.rows_total = (int32_t)rows;
+    AttnPlan mp{};
+    mp.use_mfma = 1;
+    return launch_attn_combine(m, mp, YGG_BF16, st) == hipSuccess ? YGG_OK : YGG_ERR_LAUNCH;
+}
+
+int32_t ygg_block8_append(const ygg_shape* s, int32_t n_layers, const void* k_new, const void* v_new, int32_t n_rows,
+                          const int32_t* rows, int32_t max_new, const int32_t* n_new, const int32_t* seq_lens,
+                          const ygg_block8_cache* cache, void* hip_stream) {
+    if (int32_t rc = check_block8(s)) return rc;
+    if (int32_t rc = check_cache(cache)) return rc;
+    if (!k_new || !v_new || !n_new || !seq_lens) return YGG_ERR_NULL;
+    if (n_layers < 1 || n_layers > 65535 || n_rows < 1 || max_new < 1 || (!rows && max_new > n_rows)) return YGG_ERR_SHAPE;
+    if (!aligned16(k_new) || !aligned16(v_new)) return YGG_ERR_UNSUPPORTED;
+    AppendArgs a{};
+    a.k_new = k_new; a.v_new = v_new; a.rows = rows; a.n_new = n_new; a.seq_lens = seq_lens;
+    a.k_codes = cache->k_codes; a.v_codes = cache->v_codes; a.k_scale = cache->k_scale; a.v_scale = cache->v_scale;
+    a.k_tail = cache->k_tail; a.v_tail = cache->v_tail;
+    a.nblk = (s->kv_capacity + YGG_KV_BLOCK - 1) / YGG_KV_BLOCK; a.cap = s->kv_capacity;
+    a.n_layers = n_layers; a.B = s->batch; a.Hkv = s->n_kv_heads; a.n_rows = n_rows; a.max_new = max_new;
+    a.blocks = (int32_t)(((int64_t)max_new + YGG_KV_BLOCK - 1) / YGG_KV_BLOCK);
+    if ((int64_t)n_layers * a.B * a.Hkv > 0x7fffffffLL / a.blocks) return YGG_ERR_UNSUPPORTED;
+    return launch_block8_append(a, s->head_dim, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? YGG_OK : YGG_ERR_LAUNCH;
+}
+
+int32_t ygg_tree_rotary(const ygg_shape* s, const void* q, int64_t q_stride, const void* k, int64_t k_stride, void* q_out, void* k_out,
+                        const double* frequencies, int32_t rotary_dim, int32_t interleaved, float scale, const int32_t* seq_lens,
+                        const int32_t* parent_idx, const int32_t* positions, void* hip_stream) {
+    if (!s) return YGG_ERR_NULL;
+    if (!common_shape_ok(*s)) return YGG_ERR_SHAPE;
+    if (!positions && s->n_nodes > kMaxNodes) return YGG_ERR_UNSUPPORTED;
+    if (s->kv_dtype < YGG_F32 || s->kv_dtype > YGG_FP8_BLOCK || (s->head_dim != 64 && s->head_dim != 128)) return YGG_ERR_UNSUPPORTED;
+    if ((!q && !k) || (q && !q_out) || (k && !k_out) || !frequencies || (!positions && (!seq_lens || !parent_idx))) return YGG_ERR_NULL;
+    if (rotary_dim < 16 || rotary_dim > s->head_dim || !std::isfinite(scale)) return YGG_ERR_SHAPE;
+    if (rotary_dim % 16) return YGG_ERR_UNSUPPORTED;
+    const bool f32 = s->kv_dtype == YGG_F32;
+    const int64_t q_dense = (int64_t)s->n_q_heads * s->head_dim, k_dense = (int64_t)s->n_kv_heads * s->head_dim;
+    const int64_t per16 = f32 ? 4 : 8;   // elements of 16 bytes
+    if (!q_stride) q_stride = q_dense;
+    if (!k_stride) k_stride = k_dense;
+    if ((q && (q_stride < q_dense || (q == q_out && q_stride != q_dense))) ||
+        (k && (k_stride < k_dense || (k == k_out && k_stride != k_dense)))) return YGG_ERR_SHAPE;
+    if ((q && (q_stride % per16 || !aligned16(q) || !aligned16(q_out))) || (k && (k_stride % per16 || !aligned16(k) || !aligned16(k_out))))
+        return YGG_ERR_UNSUPPORTED;
+    RotaryArgs a{};
+    a.q = q; a.k = k; a.q_out = q_out; a.k_out = k_out; a.frequencies = frequencies;
+    a.seq_lens = seq_lens; a.parent_idx = parent_idx; a.positions = positions;
+    a.q_stride = q_stride; a.k_stride = k_stride;
+    a.B = s->batch; a.N = s->n_nodes; a.Hq = q ? s->n_q_heads : 0; a.Hkv = k ? s->n_kv_heads : 0; a.Dh = s->head_dim;
+    const int64_t units = ((int64_t)a.Hq + a.Hkv) * (a.Dh / 16);
+    if (units > (1 << 22)) return YGG_ERR_UNSUPPORTED;
+    a.units = (int32_t)units;
+    a.rotary_dim = rotary_dim; a.max_seq_len = s->max_seq_len; a.scale = scale;
+    return launch_rotary(a, f32, interleaved != 0, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? YGG_OK : YGG_ERR_LAUNCH;
+}
+
+int32_t ygg_count_tokens(const ygg_shape* s, const int32_t* tokens, int32_t n_tokens, const int32_t* rows, int32_t first, int32_t max_new,
+                         const int32_t* n_new, int32_t prompt, int32_t* counts, void* hip_stream) {
+    if (int32_t rc = check_shape(s, false, true)) return rc;
+    if (!tokens || !n_new || !counts) return YGG_ERR_NULL;
+    if (n_tokens < 1 || max_new < 1 || first < 0) return YGG_ERR_SHAPE;
+    CountArgs a{};
+    a.tokens = tokens; a.rows = rows; a.n_new = n_new; a.counts = counts;
+    a.B = s->batch; a.V = s->vocab; a.n_tokens = n_tokens; a.first = first; a.max_new = max_new; a.prompt = prompt != 0;
+    return launch_count(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? YGG_OK : YGG_ERR_LAUNCH;
+}
+
+int32_t ygg_constrain_logits(const ygg_shape* s, const void* logits, int32_t logits_dtype, int64_t row_stride, const int32_t* parent_idx,
+                             const int32_t* token_ids, const ygg_logit_rules* rules, float* out, int32_t* best, void* workspace,
+                             size_t workspace_bytes, void* hip_stream) {
+    if (int32_t rc = check_shape(s, false, true)) return rc;
+    if (!logits || !parent_idx || !token_ids || !rules || (!out && !best)) return YGG_ERR_NULL;
+    if (logits_dtype != YGG_F32 && logits_dtype != YGG_BF16) return YGG_ERR_UNSUPPORTED;
+    if (!row_stride) row_stride = s->vocab;
+    if (row_stride < s->vocab) return YGG_ERR_SHAPE;
+    if (static_cast<const void*>(out) == logits && (logits_dtype != YGG_F32 || row_stride != s->vocab)) return YGG_ERR_SHAPE;
+    if (rules->masks && !rules->mask_index) return YGG_ERR_NULL;
+    if (rules->masks && rules->n_masks < 1) return YGG_ERR_SHAPE;
+    const int64_t rows = (int64_t)s->batch * s->n_nodes;
+    if (rows > 0x7fffffffLL || s->vocab > (1 << 28)) return YGG_ERR_UNSUPPORTED;   // (the launch grid)
+    if (best)
+        if (int32_t rc = check_workspace(workspace, workspace_bytes, constrain_scratch_bytes(*s))) return rc;
+    ConstrainArgs a{};
+    a.logits = logits; a.parent_idx = parent_idx; a.token_ids = token_ids; a.counts = rules->counts; a.repetition = rules->repetition;
+    a.presence = rules->presence; a.frequency = rules->frequency; a.bias = rules->bias; a.masks = rules->masks;
+    a.mask_index = rules->mask_index; a.out = out; a.best = best; a.part = workspace; a.row_stride = row_stride;
+    a.B = s->batch; a.N = s->n_nodes; a.V = s->vocab; a.bias_shared = rules->bias_shared != 0; a.n_masks = rules->n_masks;
+    return launch_constrain(a, logits_dtype == YGG_F32, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? YGG_OK : YGG_ERR_LAUNCH;
 }
 
 }  // extern "C"

@@ -156,4 +156,101 @@ AcceptPlan plan_accept(const ygg_shape& s);
 size_t accept_scratch_bytes(const ygg_shape& s);
 hipError_t launch_accept(const AcceptArgs& a, hipStream_t st);
 
+// ---- attention over the 8-bit block cache ----------------------------------------------------------
+struct Block8Plan {
+    int32_t row_blocks;   // 32-row blocks to a workgroup: 1, 2, 4 or 8
+    int32_t row_tiles;    // workgroups along the N*G query rows of one kv head
+    int32_t runs;         // equal runs of the batch's blocks per (kv head, row tile); split 0 of a sequence is its own keys
+    size_t part_o_bytes, part_rec_bytes, seq_splits_bytes;
+};
+struct Block8Args {
+    const void* q;
+    const void* k_codes;
+    const void* v_codes;
+    const float* k_scale;
+    const float* v_scale;
+    const void* k_tail;
+    const void* v_tail;
+    const void* k_tree;
+    const void* v_tree;
+    const int32_t* seq_lens;
+    const int32_t* parent_idx;
+    void* part_o;          // as in AttnArgs, matrix-core format
+    float3* part_rec;
+    int32_t* seq_splits;
+    int64_t nblk, rows_total;
+    int32_t B, N, Hq, Hkv, G, R;   // R = N * G rows share a stream
+    int32_t row_tiles, runs, max_seq_len, stat_at;
+    float scale;
+};
+Block8Plan plan_block8(const ygg_shape& s);
+hipError_t launch_attn_block8(const Block8Args& a, const Block8Plan& p, int head_dim, hipStream_t st);
+hipError_t raise_limits_attn_block8();
+
+// ---- appending to the 8-bit block cache ------------------------------------------------------------
+struct AppendArgs {
+    const void* k_new;
+    const void* v_new;
+    const int32_t* rows;
+    const int32_t* n_new;
+    const int32_t* seq_lens;
+    void* k_codes;
+    void* v_codes;
+    float* k_scale;
+    float* v_scale;
+    void* k_tail;
+    void* v_tail;
+    int64_t nblk, cap;
+    int32_t n_layers, B, Hkv, n_rows, max_new;
+    int32_t blocks;        // touched blocks that the new tokens can complete, at least 1
+};
+hipError_t launch_block8_append(const AppendArgs& a, int head_dim, hipStream_t st);
+
+// ---- rotary positions --------------------------------------------------------------------------------
+struct RotaryArgs {
+    const void* q;
+    const void* k;
+    void* q_out;
+    void* k_out;
+    const double* frequencies;
+    const int32_t* seq_lens;
+    const int32_t* parent_idx;
+    const int32_t* positions;   // or null: seq_lens + depth
+    int64_t q_stride, k_stride;
+    int32_t B, N, Hq, Hkv, Dh;  // Hq or Hkv 0: that tensor is left out
+    int32_t units;              // pieces of 16 elements of a token, (Hq + Hkv) * Dh / 16
+    int32_t rotary_dim, max_seq_len;
+    float scale;
+};
+hipError_t launch_rotary(const RotaryArgs& a, bool f32, bool interleaved, hipStream_t st);
+
+// ---- constraints on logits -----------------------------------------------------------------------------
+struct ConstrainArgs {
+    const void* logits;
+    const int32_t* parent_idx;
+    const int32_t* token_ids;
+    const int32_t* counts;
+    const float* repetition;
+    const float* presence;
+    const float* frequency;
+    const float* bias;
+    const uint32_t* masks;
+    const int32_t* mask_index;
+    float* out;
+    int32_t* best;
+    void* part;            // [B*N][chunks] {float val; int32 idx}
+    int64_t row_stride;
+    int32_t B, N, V, bias_shared, n_masks;
+};
+size_t constrain_scratch_bytes(const ygg_shape& s);
+hipError_t launch_constrain(const ConstrainArgs& a, bool f32, hipStream_t st);
+struct CountArgs {
+    const int32_t* tokens;
+    const int32_t* rows;
+    const int32_t* n_new;
+    int32_t* counts;
+    int32_t B, V, n_tokens, first, max_new, prompt;
+};
+hipError_t launch_count(const CountArgs& a, hipStream_t st);
+
 }  // namespace ygg
