@@ -204,7 +204,7 @@ def _check(rc: int, what: str):
 
 def _kv_torch_dtype(shape: Shape):
     """Element type of the K/V tensors (8-bit codes travel as uint8)."""
-    return {F32: torch.float32, BF16: torch.bfloat16, FP8_E4M3: torch.uint8}[shape.kv_dtype]
+    return {F32: torch.float32, BF16: torch.bfloat16, FP8_E4M3: torch.uint8, FP8_BLOCK: torch.bfloat16}[shape.kv_dtype]
 
 
 def _explain(shape: Shape, *checks):

@@ -76,11 +76,12 @@ __global__ __launch_bounds__(256) void constrain_kernel(ConstrainArgs a) {
     float bv = -INFINITY;
     int bi = 0x7fffffff;
     auto constrained = [&](float v, int32_t confirmed, uint32_t times, float add, bool allowed) {
+#pragma clang fp contract(off)
         const uint32_t c = ((uint32_t)confirmed & 0x7fffffffu) + times;
-        if (confirmed != 0 || times) v = v > 0.f ? __fdiv_rn(v, repetition) : __fmul_rn(v, repetition);
-        v = __fsub_rn(v, __fmul_rn(frequency, (float)c));
-        v = __fsub_rn(v, c ? presence : 0.f);
-        if (bias) v = __fadd_rn(v, add);
+        if (confirmed != 0 || times) v = v > 0.f ? v / repetition : v * repetition;
+        v = v - frequency * (float)c;
+        v = v - (c ? presence : 0.f);
+        if (bias) v = v + add;
         return allowed ? v : -INFINITY;
     };
     for (int j = c0 + 4 * tid; j < c1; j += 1024) {

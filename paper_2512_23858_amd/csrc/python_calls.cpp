@@ -116,7 +116,7 @@ struct Args {
 };
 
 at::ScalarType kv_type(const ygg_shape& s) {
-    return s.kv_dtype == YGG_F32 ? at::kFloat : s.kv_dtype == YGG_BF16 ? at::kBFloat16 : at::kByte;
+    return s.kv_dtype == YGG_F32 ? at::kFloat : s.kv_dtype == YGG_FP8_E4M3 ? at::kByte : at::kBFloat16;
 }
 
 template <typename F>
@@ -141,7 +141,7 @@ PyObject* tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!arity(n, 12)) return nullptr;
     ygg_shape s{};
     Args t{a};
-    t.ok = read_shape(a[0], s) && s.kv_dtype >= 0 && s.kv_dtype <= 2;
+    t.ok = read_shape(a[0], s) && s.kv_dtype >= 0 && s.kv_dtype <= 3;
     const at::ScalarType dt = kv_type(s);
     void *q = t.ptr(1, dt), *kc = t.ptr(2, dt), *vc = t.ptr(3, dt), *kt = t.ptr(5, dt), *vt = t.ptr(6, dt), *out = t.ptr(8, dt);
     int32_t *lens = t.ints(4), *parent = t.ints(7);
@@ -238,7 +238,7 @@ PyObject* accept_and_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!arity(n, 15)) return nullptr;
     ygg_shape s{};
     Args t{a};
-    t.ok = read_shape(a[0], s) && s.kv_dtype >= 0 && s.kv_dtype <= 2;
+    t.ok = read_shape(a[0], s) && s.kv_dtype >= 0 && s.kv_dtype <= 3;
     const at::ScalarType dt = kv_type(s);
     int32_t layers = 0;
     t.number(1, layers);
