@@ -1,6 +1,6 @@
 // Tree attention over the 8-bit block cache (include/ygg.h has the format), matrix cores throughout.
 //
-// For one (sequence, kv head) the N nodes x G query heads are R = N*G rows that share one stream of K/V.  Two kinds of workgroup:
+// For one (sequence, kv head) the N nodes x G query heads are R = N*G rows that share one stream of K/V.  Two kinds of keys:
 //
 //   blocks  the full blocks of 64 tokens, as they are stored: K and V codes go from memory to LDS by direct loads and from there as
 //           operands into v_mfma_scale_f32_32x32x64_f8f6f4.  S^T = K Q^T with a lane per query row, O^T += V^T P^T.  Widening the
@@ -12,8 +12,9 @@
 //   own     the open block's rows and the tree's own keys under the ancestor mask, bf16 as they are, v_mfma_f32_32x32x16_bf16.
 //
 // The blocks of all sequences are laid end to end and cut into equal runs, one per workgroup of a (kv head, row tile), whatever the
-// lengths; a run is served segment by segment, one for each sequence that it touches.  Every segment leaves a partial (m, l, O~) per
-// row: split 0 of a sequence is its own keys, 1 + r the r-th run that touches it.  attn_combine_kernel merges them.
+// lengths, with room for each sequence's own keys behind its blocks; a run is served segment by segment, one for each sequence that it
+// touches.  A segment that is all of its sequence writes the final rows; others leave a partial (m, l, O~) per row, and
+// attn_combine_kernel merges them.
 #include "ygg_internal.h"
 #include "ygg_device.h"
 #include "attn_common.h"
@@ -36,9 +37,9 @@ constexpr int kRescale = 30;    // a row's reference moves when a block's maximu
 template <int DH, int NW, int RB>
 struct Layout {
     static constexpr int KS = NW / RB;                    // wavefronts that share a row block deal the tiles out
-    static constexpr int TILE = 2 * kT * DH;              // bytes of a tile: K's codes, then V's
-    static constexpr int STAGE = KS * TILE;
-    static constexpr int NSTAGE = STAGE >= 65536 ? 2 : STAGE >= 32768 ? 4 : 4;
+    static constexpr int HALF = kT * DH;                  // bytes of a tile of K's (or V's) codes
+    static constexpr int STAGE = KS * 2 * HALF;           // [share][K, V]
+    static constexpr int NSTAGE = STAGE >= 65536 ? 2 : 4;
     static constexpr int OROW = DH + 4;                   // floats of a row of O~ in LDS
     static constexpr int MERGE = NW * 32 * OROW * 4;
     static constexpr int VROW = 40;                       // bf16 of a row of V^T in LDS (32 keys)
@@ -50,6 +51,36 @@ struct Layout {
     }
 };
 
+// What a workgroup accumulates for its rows: 2^ref * O~ and 2^ref * l.  A lane holds row n = lane % 32 of its wavefront's block; ref is
+// a whole number, the same in both halves of the wavefront, and l is that half's share.
+template <int DH>
+struct Rows {
+    f32x16 o[DH / 32];
+    int ref;
+    float l;
+    bool any;       // (wave-uniform) some key was seen: ref is set
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int d = 0; d < DH / 32; ++d) o[d] = f32x16{};
+        ref = 0;
+        l = 0.f;
+        any = false;
+    }
+    // c: a whole number not below the next keys' largest score (base 2), less a constant
+    __device__ __forceinline__ void refer_to(int c) {
+        if (__any(c - ref > kRescale)) {
+            const int up = max(c - ref, 0);
+            const float fix = ldexpf(1.f, -up);
+            ref += up;
+            l *= fix;
+#pragma unroll
+            for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[d][e] *= fix;
+        }
+    }
+};
+
 __device__ __forceinline__ float other_half_max(float v) {
     const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
@@ -58,13 +89,16 @@ __device__ __forceinline__ float both_halves_sum(float v) {
     const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
-// hi + lo of four values, E4M3 each
+// hi + lo of four values, E4M3 each.  A conversion writes one half of a word, so the words' old values pass through (set to nothing first,
+// they would cost a move each); the asm keeps the conversions where they are written: sunk to the words' use, in the next step behind a
+// branch, they keep their arguments in registers until then.
 __device__ __forceinline__ void split4(const float (&x)[4], int& hi, int& lo) {
-    hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], hi, false);
     hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], hi, true);
     const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
-    lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] - a[0], x[1] - a[1], 0, false);
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] - a[0], x[1] - a[1], lo, false);
     lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] - b[0], x[3] - b[1], lo, true);
+    asm volatile("" : "+v"(hi), "+v"(lo));
 }
 __device__ __forceinline__ i32x8 read_operand(const unsigned char* p) {   // the two 16-byte parts of a chunk pair, 1024 bytes apart
     const i32x4 a = *reinterpret_cast<const i32x4*>(p), b = *reinterpret_cast<const i32x4*>(p + 1024);
@@ -74,80 +108,89 @@ __device__ __forceinline__ float uniform_load(const float* p) {   // through the
     return *(const __attribute__((address_space(4))) float*)(p);
 }
 
-// Partial rows of one segment: the wavefronts that share a row block merge through LDS, and the rows leave as fp16 relative to c.
+// Rows of one segment: the wavefronts that share a row block merge through LDS; then the rows leave as a partial, fp16 relative to
+// their largest magnitude, or, where the segment is all of its sequence, as they are wanted.
 template <int DH, int NW, int RB>
-__device__ __forceinline__ void write_partial(const Block8Args& a, unsigned char* smem, float* stat, const f32x16 (&o)[DH / 32], float ref,
-                                              float l, int b, int g, int row0, int split) {
+__device__ __forceinline__ void write_rows(const Block8Args& a, unsigned char* smem, float* stat, Rows<DH>& x, int b, int g, int row0,
+                                           int split /* -1: final */) {
     using Lay = Layout<DH, NW, RB>;
     constexpr int KS = Lay::KS;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = lane & 31, half = lane >> 5;
     float* const o_s = reinterpret_cast<float*>(smem);
+    const float l = both_halves_sum(x.l);
     __syncthreads();   // the tiles are read
 #pragma unroll
     for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
             *reinterpret_cast<float4*>(o_s + (wave * 32 + n) * Lay::OROW + 32 * d + 8 * q + 4 * half) =
-                make_float4(o[d][4 * q], o[d][4 * q + 1], o[d][4 * q + 2], o[d][4 * q + 3]);
+                make_float4(x.o[d][4 * q], x.o[d][4 * q + 1], x.o[d][4 * q + 2], x.o[d][4 * q + 3]);
     if (half == 0) {
-        stat[(wave * 32 + n) * 2] = ref;
+        stat[(wave * 32 + n) * 2] = x.any ? (float)x.ref : -INFINITY;
         stat[(wave * 32 + n) * 2 + 1] = l;
     }
     __syncthreads();
     constexpr int LPR = DH / 8;   // lanes of a row
     for (int it = tid; it < RB * 32 * LPR; it += NW * 64) {
         const int r = it / LPR, col = it % LPR;
+        const int row = row0 + r;
+        if (row >= a.R) break;    // (a row's lanes go together)
         float m = -INFINITY, w[KS], sum = 0.f;
 #pragma unroll
         for (int s = 0; s < KS; ++s) m = fmaxf(m, stat[((s * RB * 32) + r) * 2]);
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-            const float x = stat[((s * RB * 32) + r) * 2];
-            w[s] = x == -INFINITY ? 0.f : exp2f(x - m);
+            const float y = stat[((s * RB * 32) + r) * 2];
+            w[s] = y == -INFINITY ? 0.f : exp2f(y - m);
             sum = fmaf(stat[((s * RB * 32) + r) * 2 + 1], w[s], sum);
         }
         float v[8] = {};
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             const float4* p = reinterpret_cast<const float4*>(o_s + (s * RB * 32 + r) * Lay::OROW + 8 * col);
-            const float4 x = p[0], y = p[1];
-            const float e[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+            const float4 y = p[0], z = p[1];
+            const float e[8] = {y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w};
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = w[s] != 0.f ? fmaf(e[k], w[s], v[k]) : v[k];
+            for (int k = 0; k < 8; ++k) v[k] = fmaf(e[k], w[s], v[k]);
         }
-        float c = 0.f;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) c = fmaxf(c, fabsf(v[k]));
-        c = fmaxf(group_reduce(c, LPR, [](float x, float y) { return fmaxf(x, y); }), 1.17549435e-38f);
-        const int row = row0 + r;
-        if (row >= a.R) continue;
         const int node = row / a.G, h = g * a.G + row % a.G;
-        const int64_t at = (int64_t)split * a.rows_total + ((int64_t)b * a.N + node) * a.Hq + h;
-        __attribute__((ext_vector_type(8))) _Float16 half8;
-        const float inv = 1.f / c;
+        const int64_t out_row = ((int64_t)b * a.N + node) * a.Hq + h;
+        if (split < 0) {
+            const float inv = 1.f / sum;
+            u32x4 y;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) half8[k] = (_Float16)(v[k] * inv);
-        *reinterpret_cast<decltype(half8)*>(static_cast<_Float16*>(a.part_o) + at * DH + 8 * col) = half8;
-        if (col == 0) a.part_rec[at] = make_float3(m, sum, c);
+            for (int k = 0; k < 4; ++k) y[k] = pack_bf16x2(v[2 * k] * inv, v[2 * k + 1] * inv);
+            *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.out) + out_row * DH + 8 * col) = y;
+            if (a.lse && col == 0) a.lse[out_row] = m * kLn2 + logf(sum);
+        } else {
+            float c = 0.f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) c = fmaxf(c, fabsf(v[k]));
+            c = fmaxf(group_reduce(c, LPR, [](float y, float z) { return fmaxf(y, z); }), 1.17549435e-38f);
+            const int64_t at = (int64_t)split * a.rows_total + out_row;
+            __attribute__((ext_vector_type(8))) _Float16 y;
+            const float inv = 1.f / c;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) y[k] = (_Float16)(v[k] * inv);
+            *reinterpret_cast<decltype(y)*>(static_cast<_Float16*>(a.part_o) + at * DH + 8 * col) = y;
+            if (col == 0) a.part_rec[at] = make_float3(m, sum, c);
+        }
     }
     __syncthreads();   // before the next segment's tiles
 }
 
-__device__ __forceinline__ int length_of(const Block8Args& a, int b) {
-    const int L = a.seq_lens[b];
-    return L < 0 ? 0 : (L > a.max_seq_len ? a.max_seq_len : L);
-}
-
+// The open block's rows and the tree's keys under the ancestor mask.
 template <int DH, int NW, int RB>
-__device__ void own_keys(const Block8Args& a, unsigned char* smem, float* stat, int b, int g, int row0) {
+__device__ __forceinline__ void own_keys(const Block8Args& a, unsigned char* smem, Rows<DH>& x, int b, int g, int row0, int L) {
     using Lay = Layout<DH, NW, RB>;
     constexpr int KS = Lay::KS, NK = DH / 16, NDB = DH / 32;
+    constexpr int PIECES = 32 * DH / 8, VP = (PIECES + RB * 64 - 1) / (RB * 64);   // of eight elements of a V tile, and to a thread
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, half = lane >> 5;
     const int rb = wave % RB, share = wave / RB;
-    const int L = length_of(a, b), open = L % kT;
+    const int open = L % kT;
     uint16_t* const vt = reinterpret_cast<uint16_t*>(smem) + share * DH * Lay::VROW;
     int32_t* const parent_s = reinterpret_cast<int32_t*>(smem + Lay::OWN);
     const int words = (a.N + 31) / 32;
@@ -155,10 +198,37 @@ __device__ void own_keys(const Block8Args& a, unsigned char* smem, float* stat, 
 
     const int row = min(row0 + rb * 32 + n, a.R - 1);
     const int node = row / a.G, h = g * a.G + row % a.G;
+    const int open_tiles = (open + 31) / 32, tree_tiles = (a.N + 31) / 32, tiles = open_tiles + tree_tiles;
+    const int64_t row_e = (int64_t)a.Hkv * DH;
+    const int64_t first = L / kT % 2 * kT;
+    const uint16_t* const k_open = static_cast<const uint16_t*>(a.k_tail) + ((int64_t)b * 2 * kT + first) * row_e + (int64_t)g * DH;
+    const uint16_t* const v_open = static_cast<const uint16_t*>(a.v_tail) + ((int64_t)b * 2 * kT + first) * row_e + (int64_t)g * DH;
+    const uint16_t* const k_tree = static_cast<const uint16_t*>(a.k_tree) + (int64_t)b * a.N * row_e + (int64_t)g * DH;
+    const uint16_t* const v_tree = static_cast<const uint16_t*>(a.v_tree) + (int64_t)b * a.N * row_e + (int64_t)g * DH;
+    auto keys_of = [&](int tile) { return tile >= tiles ? 0 : min(32, tile >= open_tiles ? a.N - (tile - open_tiles) * 32 : open - tile * 32); };
+    i32x4 k_next[NK];
+    i16x8 v_next[VP];
+    auto fetch = [&](int tile) {   // beyond the last tile: nothing
+        const int valid = keys_of(tile);
+        if (valid <= 0) return;
+        const bool in_tree = tile >= open_tiles;
+        const int64_t k0 = (in_tree ? tile - open_tiles : tile) * 32;
+        const uint16_t* const kp = (in_tree ? k_tree : k_open) + (k0 + min(n, valid - 1)) * row_e + 8 * half;
+        const uint16_t* const vp = (in_tree ? v_tree : v_open) + k0 * row_e;
+#pragma unroll
+        for (int k = 0; k < NK; ++k) k_next[k] = *reinterpret_cast<const i32x4*>(kp + 16 * k);
+#pragma unroll
+        for (int u = 0; u < VP; ++u) {
+            const int p = (rb + u * RB) * 64 + lane, key = p % 32, d = p / 32 * 8;
+            v_next[u] = i16x8{};   // keys beyond the last are zeros (0 * what lies there need not be 0)
+            if (key < valid && p < PIECES) v_next[u] = *reinterpret_cast<const i16x8*>(vp + key * row_e + d);
+        }
+    };
     i32x4 q[NK];
     const uint16_t* const qp = static_cast<const uint16_t*>(a.q) + (((int64_t)b * a.N + node) * a.Hq + h) * DH + 8 * half;
 #pragma unroll
     for (int k = 0; k < NK; ++k) q[k] = *reinterpret_cast<const i32x4*>(qp + 16 * k);
+    __syncthreads();   // the tiles of the blocks are read
     for (int j = tid; j < a.N; j += NW * 64) parent_s[j] = a.parent_idx[(int64_t)b * a.N + j];
     if (share == 0)
         for (int w = lane; w < 32 * words; w += 64) mask_s[w] = 0;
@@ -170,47 +240,28 @@ __device__ void own_keys(const Block8Args& a, unsigned char* smem, float* stat, 
             if (p < 0 || p >= j) break;
             j = p;
         }
-    __syncthreads();
-
-    const int open_tiles = (open + 31) / 32, tree_tiles = (a.N + 31) / 32, tiles = open_tiles + tree_tiles;
-    const int64_t row_e = (int64_t)a.Hkv * DH;
-    const int64_t first = L / kT % 2 * kT;
-    const uint16_t* const kt = static_cast<const uint16_t*>(a.k_tail) + ((int64_t)b * 2 * kT + first) * row_e + (int64_t)g * DH;
-    const uint16_t* const vtail = static_cast<const uint16_t*>(a.v_tail) + ((int64_t)b * 2 * kT + first) * row_e + (int64_t)g * DH;
-    const uint16_t* const ktree = static_cast<const uint16_t*>(a.k_tree) + (int64_t)b * a.N * row_e + (int64_t)g * DH;
-    const uint16_t* const vtree = static_cast<const uint16_t*>(a.v_tree) + (int64_t)b * a.N * row_e + (int64_t)g * DH;
     const float scale = a.scale * kLog2e;
-
-    f32x16 o[NDB];
-#pragma unroll
-    for (int d = 0; d < NDB; ++d) o[d] = f32x16{};
-    float m = -INFINITY, l = 0.f;
     for (int it = 0; it < tiles; it += KS) {
         const int tile = it + share;
         const bool in_tree = tile >= open_tiles;
-        const int k0 = in_tree ? (tile - open_tiles) * 32 : tile * 32;
-        const int valid = tile < tiles ? min(32, (in_tree ? a.N : open) - k0) : 0;   // keys of this tile
-        const uint16_t* const kp = (in_tree ? ktree : kt) + (int64_t)k0 * row_e;
-        const uint16_t* const vp = (in_tree ? vtree : vtail) + (int64_t)k0 * row_e;
+        const int valid = keys_of(tile);
+        fetch(tile);
         if (it > 0) __syncthreads();   // the previous V^T is read
-        if (valid > 0) {
-            // V^T by scalars: eight dimensions of a key at a time; keys beyond the last are zeros (0 * what lies there need not be 0)
-            for (int p = rb * 64 + lane; p < 32 * DH / 8; p += RB * 64) {
-                const int key = p % 32, d = p / 32 * 8;
-                i16x8 x = {};
-                if (key < valid) x = *reinterpret_cast<const i16x8*>(vp + key * row_e + d);
+        if (valid > 0)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) vt[(d + e) * Lay::VROW + key] = (uint16_t)x[e];
+            for (int u = 0; u < VP; ++u) {
+                const int p = (rb + u * RB) * 64 + lane, at = p % 32, d = p / 32 * 8;
+                if (p >= PIECES) break;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) vt[(d + e) * Lay::VROW + at] = (uint16_t)v_next[u][e];
             }
-        }
         __syncthreads();
-        if (valid <= 0) continue;
+        if (valid <= 0) continue;   // (nor any later tile)
         f32x16 s = {};
-        const uint16_t* const key = kp + (int64_t)min(n, valid - 1) * row_e + 8 * half;
 #pragma unroll
         for (int k = 0; k < NK; ++k)
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(key + 16 * k), __builtin_bit_cast(bf16x8, q[k]), s, 0, 0, 0);
-        const uint32_t seen = in_tree ? mask_s[(k0 >> 5) * 32 + n] : valid == 32 ? 0xffffffffu : (1u << valid) - 1u;
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k_next[k]), __builtin_bit_cast(bf16x8, q[k]), s, 0, 0, 0);
+        const uint32_t seen = in_tree ? mask_s[(tile - open_tiles) * 32 + n] : valid == 32 ? 0xffffffffu : (1u << valid) - 1u;
         float top = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -219,20 +270,17 @@ __device__ void own_keys(const Block8Args& a, unsigned char* smem, float* stat, 
             top = fmaxf(top, s[e]);
         }
         top = other_half_max(top);
-        const float now = fmaxf(m, top);
-        const float fix = now == -INFINITY ? 1.f : exp2f(m - now);
-        const float off = now == -INFINITY ? 0.f : now;
-        m = now;
-        l *= fix;
-#pragma unroll
-        for (int d = 0; d < NDB; ++d)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[d][e] *= fix;
+        // a row that sees none of the tile's keys keeps its reference; before it has one, any serves
+        const int c = top == -INFINITY ? (x.any ? x.ref : -(1 << 20)) : (int)ceilf(top);
+        if (!x.any) x.ref = c;
+        x.any = true;
+        x.refer_to(c);
+        const float off = (float)x.ref;
         float p[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            p[e] = exp2f(s[e] - off);
-            l += p[e];
+            p[e] = __builtin_amdgcn_exp2f(s[e] - off);
+            x.l += p[e];
         }
 #pragma unroll
         for (int k = 0; k < 2; ++k) {   // 16 keys: 16k + 4*half + {0..3, 8..11}; weights rounded to bf16 for the product
@@ -242,26 +290,52 @@ __device__ void own_keys(const Block8Args& a, unsigned char* smem, float* stat, 
 #pragma unroll
             for (int d = 0; d < NDB; ++d) {
                 const uint16_t* const v = vt + (32 * d + n) * Lay::VROW + 16 * k + 4 * half;
-                const u32x2 x = *reinterpret_cast<const u32x2*>(v), y = *reinterpret_cast<const u32x2*>(v + 8);
-                const u32x4 operand = {x[0], x[1], y[0], y[1]};
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, operand), __builtin_bit_cast(bf16x8, w), o[d], 0, 0, 0);
+                const u32x2 y = *reinterpret_cast<const u32x2*>(v), z = *reinterpret_cast<const u32x2*>(v + 8);
+                const u32x4 operand = {y[0], y[1], z[0], z[1]};
+                x.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, operand), __builtin_bit_cast(bf16x8, w), x.o[d], 0, 0, 0);
             }
         }
     }
-    l = both_halves_sum(l);
-    write_partial<DH, NW, RB>(a, smem, stat, o, m, l, b, g, row0, 0);
 }
 
+// Blocks t0 .. t1 - 1 of one stream.
 template <int DH, int NW, int RB>
-__device__ void cache_blocks(const Block8Args& a, unsigned char* smem, float* stat, int b, int g, int row0, int t0, int t1, int split) {
+__device__ __forceinline__ void cache_blocks(const Block8Args& a, unsigned char* smem, Rows<DH>& x, int b, int g, int row0, int t0, int t1) {
     using Lay = Layout<DH, NW, RB>;
     constexpr int KS = Lay::KS, J = DH / 64, NDB = DH / 32;
-    constexpr int LOADS = Lay::TILE / 1024 / RB;   // direct loads of a wavefront for its share of a tile
+    constexpr int CH = Lay::HALF / 1024;           // chunks of a tile of K
+    constexpr int LOADS = 2 * CH / RB;             // direct loads of a wavefront per tile, of K and V
     constexpr int AHEAD = Lay::NSTAGE - 1;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, half = lane >> 5;
     const int rb = wave % RB, share = wave / RB;
+
+    const int64_t stream = ((int64_t)b * a.Hkv + g) * a.nblk;
+    const int tiles = t1 - t0, steps = (tiles + KS - 1) / KS;
+    const int mine = (tiles - share + KS - 1) / KS;   // this share's tiles: share, share + KS, ..
+    const unsigned char* const kc = static_cast<const unsigned char*>(a.k_codes) + stream * kT * DH;
+    const unsigned char* const vc = static_cast<const unsigned char*>(a.v_codes) + stream * kT * DH;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem + share * 2 * Lay::HALF;
+    auto stage_of = [](int step) { return (step & (Lay::NSTAGE - 1)) * Lay::STAGE; };
+    auto tile_of = [&](int step) { return t0 + min(step * KS + share, tiles - 1); };   // beyond the last tile that one again: counts stay
+    // A step has the scores of the next tile, the weights of its own and the product of the one before: K runs two steps ahead of V.
+    auto fill = [&](int k_step, int v_step) {
+        const unsigned char* const kb = kc + (int64_t)tile_of(k_step) * Lay::HALF;
+        const unsigned char* const vb = vc + (int64_t)tile_of(max(v_step, 0)) * Lay::HALF;
+        const uint32_t to_k = lds0 + stage_of(k_step), to_v = lds0 + stage_of(v_step) + Lay::HALF;
+#pragma unroll
+        for (int c = 0; c < LOADS; ++c) {
+            if constexpr (CH % RB == 0) {
+                const int chunk = (c % (LOADS / 2)) * RB + rb;
+                if (c < LOADS / 2) dma_load16<false, 0>(kb + chunk * 1024, (uint32_t)lane * 16, to_k + chunk * 1024);
+                else dma_load16<false, 0>(vb + chunk * 1024, (uint32_t)lane * 16, to_v + chunk * 1024);
+            } else {   // twice as many wavefronts as chunks: K's, then V's
+                const int chunk = rb % CH;
+                dma_load16<false, 0>((rb < CH ? kb : vb) + chunk * 1024, (uint32_t)lane * 16, (rb < CH ? to_k : to_v) + chunk * 1024);
+            }
+        }
+    };
 
     // Q: this lane's row, dimensions 64 j + 32 half .. + 31
     const int row = min(row0 + rb * 32 + n, a.R - 1);
@@ -290,118 +364,142 @@ __device__ void cache_blocks(const Block8Args& a, unsigned char* smem, float* st
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const uint32_t u = raw[k][2 * e], v = raw[k][2 * e + 1];
-                const float x[4] = {__uint_as_float(u << 16) * by, __uint_as_float(u & 0xffff0000u) * by, __uint_as_float(v << 16) * by,
+                const float y[4] = {__uint_as_float(u << 16) * by, __uint_as_float(u & 0xffff0000u) * by, __uint_as_float(v << 16) * by,
                                     __uint_as_float(v & 0xffff0000u) * by};
-                int hi, lo;
-                split4(x, hi, lo);
+                int hi = 0, lo = 0;
+                split4(y, hi, lo);
                 qhi[j][2 * k + e] = hi;
                 qlo[j][2 * k + e] = lo;
             }
     }
 
-    const int64_t stream = ((int64_t)b * a.Hkv + g) * a.nblk;
-    const int tiles = t1 - t0, steps = (tiles + KS - 1) / KS;
-    const unsigned char* const kc = static_cast<const unsigned char*>(a.k_codes) + stream * kT * DH;
-    const unsigned char* const vc = static_cast<const unsigned char*>(a.v_codes) + stream * kT * DH;
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
-    auto fill = [&](int step) {   // this wavefront's loads of its share's tile; beyond the last tile that one again, so that counts stay
-        const int t = t0 + min(step * KS + share, tiles - 1);
-        const unsigned char* const kb = kc + (int64_t)t * kT * DH;
-        const unsigned char* const vb = vc + (int64_t)t * kT * DH;
-        const uint32_t to = lds0 + (step % Lay::NSTAGE) * Lay::STAGE + share * Lay::TILE;
-#pragma unroll
-        for (int c = 0; c < LOADS; ++c) {
-            const int chunk = rb * LOADS + c;   // K's chunks, then V's
-            const unsigned char* const src = chunk < kT * DH / 1024 ? kb + chunk * 1024 : vb + (chunk - kT * DH / 1024) * 1024;
-            dma_load16<false, 0>(src, (uint32_t)lane * 16, to + chunk * 1024);
-        }
+    const unsigned char* const lane_at = smem + share * 2 * Lay::HALF + lane * 16;
+    auto k_at = [&](int step) { return lane_at + stage_of(step); };
+    auto v_at = [&](int step) { return lane_at + stage_of(step) + Lay::HALF; };
+    struct Weights {     // of a tile's 64 keys: sum of two E4M3 values, times 2^(c - ref); ve: V's power of two
+        i32x8 hi, lo;
+        int c, ve;
     };
-    dma_wait_keep<0>();
-    for (int s = 0; s < AHEAD; ++s) fill(s);
+    auto meet = [&] {   // a private tile needs no meeting
+        if constexpr (RB > 1) lds_barrier();
+        else __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+    };
 
-    f32x16 o[NDB];
+    dma_wait_keep<0>();
 #pragma unroll
-    for (int d = 0; d < NDB; ++d) o[d] = f32x16{};
-    int ref = 0;
-    float l = 0.f;
-    bool any = false;
+    for (int c = 0; c < LOADS; ++c)
+        if (c * RB + rb < CH)
+            dma_load16<false, 0>(kc + (int64_t)tile_of(0) * Lay::HALF + (c * RB + rb) * 1024, (uint32_t)lane * 16, lds0 + (c * RB + rb) * 1024);
+    for (int i = 0; i < AHEAD; ++i) fill(i + 1, i - 1);
+    dma_wait_keep<AHEAD * LOADS>();
+    meet();
     const float scale = a.scale * kLog2e;
-    for (int step = 0; step < steps; ++step) {
-        const int t = t0 + step * KS + share;
-        const bool mine = t < t1;
-        const float ks = uniform_load(a.k_scale + stream + min(t, t1 - 1)), vs = uniform_load(a.v_scale + stream + min(t, t1 - 1));
+    auto advance = [&](int step, f32x16 (&s)[2], f32x16 (&next)[2], const Weights& old, Weights& w) {
+        const int t = tile_of(step);
+        const float ks = uniform_load(a.k_scale + stream + t), vs = uniform_load(a.v_scale + stream + t);
         dma_wait_keep<(AHEAD - 1) * LOADS>();
-        lds_barrier();
-        fill(step + AHEAD);
-        if (!mine) continue;
-        const unsigned char* const tile = smem + (step % Lay::NSTAGE) * Lay::STAGE + share * Lay::TILE + lane * 16;
-        f32x16 s[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            s[u] = f32x16{};
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const i32x8 k = read_operand(tile + (u * J + j) * 2048);
-                s[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, qhi[j], s[u], 0, 0, 0, 127, 0, qscale[j]);
-                s[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, qlo[j], s[u], 0, 0, 0, 127, 0, qscale[j]);
-            }
-        }
+        meet();
+        fill(step + 1 + AHEAD, step - 1 + AHEAD);
         float top = -INFINITY;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
         top = other_half_max(top);
+        const bool there = step < mine;        // (uniform) beyond this share's last tile all weights are zero
         const float by = ks * scale;
-        const int c = (int)ceilf(top * by) - kHeadroom;
-        if (!any) ref = c;
-        any = true;
-        if (__any(c - ref > kRescale)) {
-            const int up = max(c - ref, 0);
-            const float fix = ldexpf(1.f, -up);
-            ref += up;
-            l *= fix;
-#pragma unroll
-            for (int d = 0; d < NDB; ++d)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[d][e] *= fix;
-        }
+        w.c = there ? (int)ceilf(top * by) - kHeadroom : x.ref;
+        if (step == 0) x.ref = w.c;
+        x.refer_to(w.c);
         // v_scale = significand * 2^ve: the significand joins the weights, the power is V's block scale
         const uint32_t vb = __float_as_uint(vs);
-        const int ve = (int)(vb >> 23) & 255;
+        w.ve = (int)(vb >> 23) & 255;
         const float significand = __uint_as_float((vb & 0x7fffffu) | 0x3f800000u);
-        const float off = __builtin_amdgcn_logf(significand) - (float)c;
-        const int pscale = max(c - ref + 127, 0);
-        i32x8 phi, plo;
+        const float off = there ? __builtin_amdgcn_logf(significand) - (float)w.c : -INFINITY;
+        // 2 J products K Q of the next tile and DH / 32 products V P of the one before take turns, two matrix instructions (hi, lo) each,
+        // and this tile's weights are formed between them: a matrix instruction takes as long as 16 vector ones.  The order is the
+        // program's (sched_barrier): left to itself the compiler issues them in a row, and both wavefronts of a SIMD wait for the
+        // matrix pipe at once and then for the vector one.
+        constexpr int UNITS = 2 * J + NDB, GROUPS = 8 / UNITS;   // groups of four weights to a unit
+        const unsigned char *const kp = k_at(step + 1), *const vp = v_at(step - 1);
+        const int scale_old = max(old.c - x.ref + 127, 0);
+        next[0] = f32x16{};
+        next[1] = f32x16{};
+        auto operand = [&](int unit) { return unit % 2 == 0 ? read_operand(kp + unit / 2 * 2048) : read_operand(vp + unit / 2 * 2048); };
+        i32x8 op = operand(0);
         float sum = 0.f;
+        static_for<0, UNITS>([&](auto unit) {
+            constexpr int U = unit, I = U / 2;
+            constexpr bool QK = U % 2 == 0;
+            constexpr int u = I / J, j = I % J;      // K: half of the tile, 64 dimensions
+            i32x8 after;
+            if constexpr (U + 1 < UNITS) after = operand(U + 1);
+            float p[GROUPS][4];
+            if constexpr (QK) next[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(op, qhi[j], next[u], 0, 0, 0, 127, 0, qscale[j]);
+            else x.o[I] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(op, old.hi, x.o[I], 0, 0, 0, old.ve, 0, scale_old);
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                float p[4];
+            for (int k = 0; k < GROUPS; ++k)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    p[e] = __builtin_amdgcn_exp2f(fmaf(s[u][4 * q + e], by, off));
-                    sum += p[e];
+                    const int at = (U * GROUPS + k) * 4 + e;
+                    p[k][e] = __builtin_amdgcn_exp2f(fmaf(s[at / 16][at % 16], by, off));
                 }
-                int hi, lo;
-                split4(p, hi, lo);
-                phi[4 * u + q] = hi;
-                plo[4 * u + q] = lo;
-            }
-        l = fmaf(sum, ldexpf(1.f / significand, max(c - ref, -127)), l);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (QK) next[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(op, qlo[j], next[u], 0, 0, 0, 127, 0, qscale[j]);
+            else x.o[I] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(op, old.lo, x.o[I], 0, 0, 0, old.ve, 0, scale_old);
 #pragma unroll
-        for (int d = 0; d < NDB; ++d) {
-            const i32x8 v = read_operand(tile + kT * DH + d * 2048);
-            o[d] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(v, phi, o[d], 0, 0, 0, ve, 0, pscale);
-            o[d] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(v, plo, o[d], 0, 0, 0, ve, 0, pscale);
+            for (int k = 0; k < GROUPS; ++k) {
+                int hi = w.hi[U * GROUPS + k], lo = w.lo[U * GROUPS + k];
+                split4(p[k], hi, lo);
+                w.hi[U * GROUPS + k] = hi;
+                w.lo[U * GROUPS + k] = lo;
+                sum += (p[k][0] + p[k][1]) + (p[k][2] + p[k][3]);
+            }
+            op = after;
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        x.l = fmaf(sum, ldexpf(1.f / significand, max(w.c - x.ref, -127)), x.l);
+        // the products stay in this step too, and are not moved behind the next one's branch
+#pragma unroll
+        for (int u = 0; u < 2; ++u) asm volatile("" : "+v"(next[u]));
+#pragma unroll
+        for (int d = 0; d < NDB; ++d) asm volatile("" : "+v"(x.o[d]));
+    };
+    f32x16 s0[2], s1[2];
+    Weights w0, w1;
+    w0.hi = w0.lo = w1.hi = w1.lo = i32x8{};
+    w1.c = 0;
+    w1.ve = 127;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        s0[u] = f32x16{};
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const i32x8 k = read_operand(k_at(0) + (u * J + j) * 2048);
+            s0[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, qhi[j], s0[u], 0, 0, 0, 127, 0, qscale[j]);
+            s0[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, qlo[j], s0[u], 0, 0, 0, 127, 0, qscale[j]);
         }
     }
+    int step = 0;
+    for (; step < steps; step += 2) {
+        advance(step, s0, s1, w1, w0);
+        advance(step + 1, s1, s0, w0, w1);
+    }
     dma_wait_keep<0>();
-    l = both_halves_sum(l);
-    write_partial<DH, NW, RB>(a, smem, stat, o, any ? (float)ref : -INFINITY, l, b, g, row0, split);
+    meet();
+    x.any = mine > 0;
+    const int last = max(w1.c - x.ref + 127, 0);
+#pragma unroll
+    for (int d = 0; d < NDB; ++d) {
+        const i32x8 v = read_operand(v_at(step - 1) + d * 2048);
+        x.o[d] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(v, w1.hi, x.o[d], 0, 0, 0, w1.ve, 0, last);
+        x.o[d] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(v, w1.lo, x.o[d], 0, 0, 0, w1.ve, 0, last);
+    }
 }
 
+// The batch laid end to end, in units of a block's time: of each sequence kLead empty units (what a segment costs beside its keys), its
+// full blocks, and a.own units for its own keys.  Run r of a.runs has the units r * per .. (r + 1) * per - 1 and the own keys whose middle
+// lies there, or in the run after the sequence's last block where that is further on.
 template <int DH, int NW, int RB>
 __global__ __launch_bounds__(NW * 64, NW / 4) void attn_block8_kernel(Block8Args a) {
     extern __shared__ __align__(16) unsigned char smem[];
@@ -410,26 +508,44 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_block8_kernel(Block8Args
     const int xcd = blockIdx.x % 8, rest = blockIdx.x / 8;
     const int row0 = rest % a.row_tiles * RB * 32;
     const int stream = rest / a.row_tiles * 8 + xcd;
-    const int own = a.B * a.Hkv;
-    if (stream >= own + a.runs * a.Hkv) return;
-    if (stream < own) {
-        own_keys<DH, NW, RB>(a, smem, stat, stream / a.Hkv, stream % a.Hkv, row0);
-        return;
-    }
-    const int run = (stream - own) / a.Hkv, g = (stream - own) % a.Hkv;
-    int64_t total = 0;
-    for (int b = 0; b < a.B; ++b) total += length_of(a, b) / kT;
-    const int64_t per = max((total + a.runs - 1) / a.runs, (int64_t)1);
-    const int64_t r0 = run * per, r1 = min(r0 + per, total);
-    int64_t at = 0;
-    for (int b = 0; b < a.B; ++b) {
-        const int blocks = length_of(a, b) / kT;
-        // the run that writes how many splits a sequence has: its first kv head's and row tile's run 0
-        if (run == 0 && g == 0 && row0 == 0 && threadIdx.x == 0)
-            a.seq_splits[b] = 1 + (blocks ? (int)((at + blocks - 1) / per - at / per + 1) : 0);
-        const int64_t s0 = max(r0, at), s1 = min(r1, at + blocks);
-        if (s0 < s1) cache_blocks<DH, NW, RB>(a, smem, stat, b, g, row0, (int)(s0 - at), (int)(s1 - at), 1 + (int)(run - at / per));
-        at += blocks;
+    if (stream >= a.runs * a.Hkv) return;
+    const int run = stream / a.Hkv, g = stream % a.Hkv;
+    const int lane = threadIdx.x & 63;
+    auto length = [&](int b) {
+        const int L = b < a.B ? a.seq_lens[b] : 0;
+        return L < 0 ? 0 : (L > a.max_seq_len ? a.max_seq_len : L);
+    };
+    int L = length(lane);
+    int total = wave_sum_i32(L / kT);
+    for (int b0 = 64; b0 < a.B; b0 += 64) total += wave_sum_i32(length(b0 + lane) / kT);
+    total += a.B * (a.lead + a.own);
+    const int per = (total + a.runs - 1) / a.runs;
+    int before = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        if (b0 > 0) L = length(b0 + lane);
+        const int blocks = L / kT, units = b0 + lane < a.B ? a.lead + blocks + a.own : 0;
+        const int sums = wave_prefix_i32(units, lane);
+        const int first = before + sums - units + a.lead;            // unit of the first block
+        before += __builtin_amdgcn_readlane(sums, 63);
+        int first_run = first / per, own_run = (first + blocks + a.own / 2) / per;
+        if (blocks > 0) own_run = min(own_run, (first + blocks - 1) / per + 1);
+        else first_run = own_run;
+        const int splits = own_run - first_run + 1;
+        if (run == 0 && g == 0 && row0 == 0 && threadIdx.x < 64 && units > 0) a.seq_splits[b0 + lane] = splits > 1 ? splits : 0;
+        uint64_t todo = __ballot(units > 0 && run >= first_run && run <= own_run);
+        while (todo) {
+            const int i = __builtin_ctzll(todo);
+            todo &= todo - 1;
+            const int at = __builtin_amdgcn_readlane(first, i), nb = __builtin_amdgcn_readlane(blocks, i);
+            const int t0 = max(run * per - at, 0), t1 = min((run + 1) * per - at, nb);
+            const bool own = run == __builtin_amdgcn_readlane(own_run, i);
+            const int split = run - __builtin_amdgcn_readlane(first_run, i);
+            Rows<DH> x;
+            x.clear();
+            if (t0 < t1) cache_blocks<DH, NW, RB>(a, smem, x, b0 + i, g, row0, t0, t1);
+            if (own) own_keys<DH, NW, RB>(a, smem, x, b0 + i, g, row0, __builtin_amdgcn_readlane(L, i));
+            write_rows<DH, NW, RB>(a, smem, stat, x, b0 + i, g, row0, __builtin_amdgcn_readlane(splits, i) > 1 ? split : -1);
+        }
     }
 }
 
@@ -444,7 +560,7 @@ hipError_t launch(Block8Args a, hipStream_t st) {
     const size_t smem = Layout<DH, NW, RB>::smem(a.N);
     if (smem > kAttnMfmaMaxSmem) return hipErrorInvalidValue;
     a.stat_at = (int32_t)(smem - Layout<DH, NW, RB>::STAT);
-    const int64_t streams = (int64_t)a.B * a.Hkv + (int64_t)a.runs * a.Hkv;
+    const int64_t streams = (int64_t)a.runs * a.Hkv;
     const dim3 grid((unsigned)((streams + 7) / 8 * 8 * a.row_tiles));
     hipLaunchKernelGGL((attn_block8_kernel<DH, NW, RB>), grid, dim3(NW * 64), smem, st, a);
     return hipGetLastError();

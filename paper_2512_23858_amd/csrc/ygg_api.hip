@@ -278,14 +278,22 @@ Block8Plan plan_block8(const ygg_shape& s) {
     const int64_t R = (int64_t)s.n_nodes * (s.n_q_heads / s.n_kv_heads);
     p.row_blocks = R <= 32 ? 1 : R <= 64 ? 2 : R <= 128 ? 4 : 8;
     p.row_tiles = (int32_t)((R + p.row_blocks * 32 - 1) / (p.row_blocks * 32));
-    const int64_t per_stream = (int64_t)s.n_kv_heads * p.row_tiles;
-    const int64_t at_once = 256 / per_stream;                      // one workgroup to a compute unit
-    const int64_t tiles = (int64_t)s.batch * (s.max_seq_len / YGG_KV_BLOCK);
-    int64_t runs = std::max(at_once - s.batch, at_once / 2);
-    runs = std::min(runs, tiles);
-    p.runs = (int32_t)std::clamp(runs, (int64_t)1, (int64_t)63);   // the merge takes 64 splits, one is the sequence's own keys
-    p.part_o_bytes = part_o_bytes(s, true, p.runs + 1);
-    p.part_rec_bytes = part_rec_bytes(s, p.runs + 1);
+    p.lead = 2;
+    p.own = 2 + (s.n_nodes + 31) / 32;
+    // Runs: as many as fill the chip with whole rounds of workgroups (one to a compute unit), and of one to four rounds those that take
+    // least time, a round being the units of a run and a start.
+    const int64_t at_once = std::max(streams_at_once(p.row_tiles), (int64_t)1);
+    const int64_t units = (int64_t)s.batch * (s.max_seq_len / YGG_KV_BLOCK + p.lead + p.own);
+    int64_t best = 0;
+    for (int64_t rounds = 1; rounds <= 4; ++rounds) {
+        const int64_t runs = std::clamp(rounds * at_once / s.n_kv_heads, (int64_t)1, std::min((int64_t)64, units));
+        const int64_t need = (runs * s.n_kv_heads + at_once - 1) / at_once;
+        const int64_t time = need * ((units + runs - 1) / runs + 4);
+        if (rounds == 1 || time < best) { best = time; p.runs = (int32_t)runs; }
+        p.most_runs = (int32_t)runs;
+    }
+    p.part_o_bytes = part_o_bytes(s, true, p.runs);
+    p.part_rec_bytes = part_rec_bytes(s, p.runs);
     p.seq_splits_bytes = align256((size_t)s.batch * sizeof(int32_t));
     return p;
 }
@@ -369,8 +377,8 @@ size_t ygg_workspace_bytes(const ygg_shape* s, int32_t op, int32_t n_layers) {
         }
         case YGG_OP_ATTENTION_BLOCK8: {
             if (check_block8(s) != YGG_OK) return 0;
-            const Block8Plan p = plan_block8(*s);
-            return p.part_o_bytes + p.part_rec_bytes + p.seq_splits_bytes;
+            const Block8Plan p = plan_block8(*s);   // the most runs that this or a shorter bound may take
+            return part_o_bytes(*s, true, p.most_runs) + part_rec_bytes(*s, p.most_runs) + p.seq_splits_bytes;
         }
         case YGG_OP_CONSTRAIN: {
             if (check_shape(s, false, true) != YGG_OK) return 0;
@@ -595,8 +603,9 @@ int32_t ygg_tree_attention_block8(const ygg_shape* s, const void* q, const ygg_b
     if (!aligned16(q) || !aligned16(k_tree) || !aligned16(v_tree) || !aligned16(out)) return YGG_ERR_UNSUPPORTED;
     const int64_t rows = (int64_t)s->batch * s->n_nodes * s->n_q_heads;
     const Block8Plan p = plan_block8(*s);
-    // the kernels count query rows, and workgroups, with 31 bits
-    if (rows > 0x7fffffffLL || ((int64_t)s->batch + p.runs + 8) * s->n_kv_heads * p.row_tiles > 0x7fffffffLL) return YGG_ERR_UNSUPPORTED;
+    // the kernels count query rows, workgroups and a batch's blocks with 31 bits
+    if (rows > 0x7fffffffLL || ((int64_t)p.runs + 8) * s->n_kv_heads * p.row_tiles > 0x7fffffffLL ||
+        (int64_t)s->batch * (s->max_seq_len / YGG_KV_BLOCK + p.lead + p.own) > 0x3fffffffLL) return YGG_ERR_UNSUPPORTED;
     if (int32_t rc = check_workspace(workspace, workspace_bytes, p.part_o_bytes + p.part_rec_bytes + p.seq_splits_bytes)) return rc;
     if (int32_t rc = ensure_device_ready()) return rc;
 
@@ -610,13 +619,15 @@ int32_t ygg_tree_attention_block8(const ygg_shape* s, const void* q, const ygg_b
     a.nblk = (s->kv_capacity + YGG_KV_BLOCK - 1) / YGG_KV_BLOCK;
     a.rows_total = rows;
     a.B = s->batch; a.N = s->n_nodes; a.Hq = s->n_q_heads; a.Hkv = s->n_kv_heads; a.G = a.Hq / a.Hkv; a.R = a.N * a.G;
-    a.row_tiles = p.row_tiles; a.runs = p.runs; a.max_seq_len = s->max_seq_len; a.scale = s->softmax_scale;
+    a.out = out; a.lse = lse;
+    a.row_tiles = p.row_tiles; a.runs = p.runs; a.lead = p.lead; a.own = p.own; a.max_seq_len = s->max_seq_len; a.scale = s->softmax_scale;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (launch_attn_block8(a, p, s->head_dim, st) != hipSuccess) return YGG_ERR_LAUNCH;
+    if (p.runs == 1) return YGG_OK;   // every sequence is one segment
 
     AttnArgs m{};      // the merge of the splits, shared with the other matrix-core kernels
     m.part_o = a.part_o; m.part_rec = a.part_rec; m.seq_splits = a.seq_splits; m.out = out; m.lse = lse;
-    m.B = a.B; m.N = a.N; m.Hq = a.Hq; m.Hkv = a.Hkv; m.Dh = s->head_dim; m.nsplit = p.runs + 1; m.rows_total = (int32_t)rows;
+    m.B = a.B; m.N = a.N; m.Hq = a.Hq; m.Hkv = a.Hkv; m.Dh = s->head_dim; m.nsplit = p.runs; m.rows_total = (int32_t)rows;
     AttnPlan mp{};
     mp.use_mfma = 1;
     return launch_attn_combine(m, mp, YGG_BF16, st) == hipSuccess ? YGG_OK : YGG_ERR_LAUNCH;
