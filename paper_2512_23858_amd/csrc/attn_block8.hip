@@ -14,7 +14,7 @@
 // The blocks of all sequences are laid end to end and cut into equal runs, one per workgroup of a (kv head, row tile), whatever the
 // lengths, with room for each sequence's own keys behind its blocks; a run is served segment by segment, one for each sequence that it
 // touches.  A segment that is all of its sequence writes the final rows; others leave a partial (m, l, O~) per row, and
-// attn_combine_kernel merges them.
+// block8_merge_kernel merges them.
 #include "ygg_internal.h"
 #include "ygg_device.h"
 #include "attn_common.h"
@@ -29,6 +29,7 @@ namespace {
 
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 typedef __attribute__((ext_vector_type(4))) int i32x4;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 
 constexpr int kT = YGG_KV_BLOCK;
 constexpr int kHeadroom = 7;    // weights of a block reach 2^7 (times v_scale's significand, below 2): E4M3 ends at 448
@@ -37,17 +38,19 @@ constexpr int kRescale = 30;    // a row's reference moves when a block's maximu
 template <int DH, int NW, int RB>
 struct Layout {
     static constexpr int KS = NW / RB;                    // wavefronts that share a row block deal the tiles out
-    static constexpr int HALF = kT * DH;                  // bytes of a tile of K's (or V's) codes
+    static constexpr int HALF = kT * DH;                  // bytes of a tile's K (or V): 64 rows of codes, or 32 of bf16
+    static constexpr int CHUNKS = HALF / 1024;            // a direct load of a wavefront brings 1024 bytes
+    static constexpr int LOADS = 2 * CHUNKS / RB;         // direct loads of a wavefront per tile
     static constexpr int STAGE = KS * 2 * HALF;           // [share][K, V]
     static constexpr int NSTAGE = STAGE >= 65536 ? 2 : 4;
+    static constexpr int AHEAD = NSTAGE - 1;              // tiles in flight
     static constexpr int OROW = DH + 4;                   // floats of a row of O~ in LDS
-    static constexpr int MERGE = NW * 32 * OROW * 4;
-    static constexpr int VROW = 40;                       // bf16 of a row of V^T in LDS (32 keys)
-    static constexpr int OWN = KS * DH * VROW * 2;        // own keys: V^T tiles, then parents, then masks
+    static constexpr int MERGE = NW * 32 * OROW * 4;      // in the tiles' place
     static constexpr int STAT = NW * 32 * 2 * 4;          // (reference, sum) of every wavefront's rows, behind everything else
-    static int own_bytes(int nodes) { return OWN + nodes * 4 + RB * 32 * ((nodes + 31) / 32) * 4; }
+    static constexpr int TREE = NSTAGE * STAGE;           // parents, then masks, behind the tiles
     static size_t smem(int nodes) {
-        return (size_t)std::max(std::max(NSTAGE * STAGE, MERGE), (own_bytes(nodes) + 15) / 16 * 16) + STAT;
+        const int tree = TREE + nodes * 4 + RB * 32 * ((nodes + 31) / 32) * 4;
+        return (size_t)(std::max(MERGE, tree) + 15) / 16 * 16 + STAT;
     }
 };
 
@@ -81,6 +84,20 @@ struct Rows {
     }
 };
 
+// The kernel's arguments, and the lane, as a phase of a segment first sees them: left to itself the compiler forms what depends on them
+// once for all segments and keeps it in registers that the phases need (43 of them spilled).
+typedef const __attribute__((address_space(4))) Block8Args Args;
+__device__ __forceinline__ Args& arguments() {
+    Args* p = (Args*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *p;
+}
+__device__ __forceinline__ int thread_index() {
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t;
+}
+
 __device__ __forceinline__ float other_half_max(float v) {
     const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
@@ -111,11 +128,12 @@ __device__ __forceinline__ float uniform_load(const float* p) {   // through the
 // Rows of one segment: the wavefronts that share a row block merge through LDS; then the rows leave as a partial, fp16 relative to
 // their largest magnitude, or, where the segment is all of its sequence, as they are wanted.
 template <int DH, int NW, int RB>
-__device__ __forceinline__ void write_rows(const Block8Args& a, unsigned char* smem, float* stat, Rows<DH>& x, int b, int g, int row0,
+__device__ __forceinline__ void write_rows(unsigned char* smem, float* stat, Rows<DH>& x, int b, int g, int row0,
                                            int split /* -1: final */) {
+    Args& a = arguments();
     using Lay = Layout<DH, NW, RB>;
     constexpr int KS = Lay::KS;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = thread_index(), lane = tid & 63, wave = tid >> 6;
     const int n = lane & 31, half = lane >> 5;
     float* const o_s = reinterpret_cast<float*>(smem);
     const float l = both_halves_sum(x.l);
@@ -169,67 +187,66 @@ __device__ __forceinline__ void write_rows(const Block8Args& a, unsigned char* s
             for (int k = 0; k < 8; ++k) c = fmaxf(c, fabsf(v[k]));
             c = fmaxf(group_reduce(c, LPR, [](float y, float z) { return fmaxf(y, z); }), 1.17549435e-38f);
             const int64_t at = (int64_t)split * a.rows_total + out_row;
-            __attribute__((ext_vector_type(8))) _Float16 y;
+            f16x8 y;
             const float inv = 1.f / c;
 #pragma unroll
             for (int k = 0; k < 8; ++k) y[k] = (_Float16)(v[k] * inv);
-            *reinterpret_cast<decltype(y)*>(static_cast<_Float16*>(a.part_o) + at * DH + 8 * col) = y;
+            *reinterpret_cast<f16x8*>(static_cast<_Float16*>(a.part_o) + at * DH + 8 * col) = y;
             if (col == 0) a.part_rec[at] = make_float3(m, sum, c);
         }
     }
     __syncthreads();   // before the next segment's tiles
 }
 
-// The open block's rows and the tree's keys under the ancestor mask.
-template <int DH, int NW, int RB>
-__device__ __forceinline__ void own_keys(const Block8Args& a, unsigned char* smem, Rows<DH>& x, int b, int g, int row0, int L) {
+// The open block's rows and the tree's keys under the ancestor mask, 32 to a tile.  Tiles come in by direct loads, 16-byte slots permuted
+// within a row so that operand reads meet no bank twice: K slot ^ row, V slot ^ 4 (row % (DH / 32)).
+template <int DH, int NW, int RB, bool NT>
+__device__ __forceinline__ void own_keys(unsigned char* smem, Rows<DH>& x, int b, int g, int row0, int L) {
+    Args& a = arguments();
     using Lay = Layout<DH, NW, RB>;
-    constexpr int KS = Lay::KS, NK = DH / 16, NDB = DH / 32;
-    constexpr int PIECES = 32 * DH / 8, VP = (PIECES + RB * 64 - 1) / (RB * 64);   // of eight elements of a V tile, and to a thread
-    const int tid = threadIdx.x, lane = tid & 63;
+    constexpr int KS = Lay::KS, NK = DH / 16, NDB = DH / 32, ROWB = 2 * DH, SLOTS = ROWB / 16, RPI = 1024 / ROWB;
+    const int tid = thread_index(), lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, half = lane >> 5;
     const int rb = wave % RB, share = wave / RB;
     const int open = L % kT;
-    uint16_t* const vt = reinterpret_cast<uint16_t*>(smem) + share * DH * Lay::VROW;
-    int32_t* const parent_s = reinterpret_cast<int32_t*>(smem + Lay::OWN);
+    const bool active = row0 + rb * 32 < a.R;
+    int32_t* const parent_s = reinterpret_cast<int32_t*>(smem + Lay::TREE);
     const int words = (a.N + 31) / 32;
     uint32_t* const mask_s = reinterpret_cast<uint32_t*>(parent_s + a.N) + rb * 32 * words;   // [word][row of the row block]
 
-    const int row = min(row0 + rb * 32 + n, a.R - 1);
-    const int node = row / a.G, h = g * a.G + row % a.G;
-    const int open_tiles = (open + 31) / 32, tree_tiles = (a.N + 31) / 32, tiles = open_tiles + tree_tiles;
-    const int64_t row_e = (int64_t)a.Hkv * DH;
-    const int64_t first = L / kT % 2 * kT;
-    const uint16_t* const k_open = static_cast<const uint16_t*>(a.k_tail) + ((int64_t)b * 2 * kT + first) * row_e + (int64_t)g * DH;
-    const uint16_t* const v_open = static_cast<const uint16_t*>(a.v_tail) + ((int64_t)b * 2 * kT + first) * row_e + (int64_t)g * DH;
-    const uint16_t* const k_tree = static_cast<const uint16_t*>(a.k_tree) + (int64_t)b * a.N * row_e + (int64_t)g * DH;
-    const uint16_t* const v_tree = static_cast<const uint16_t*>(a.v_tree) + (int64_t)b * a.N * row_e + (int64_t)g * DH;
-    auto keys_of = [&](int tile) { return tile >= tiles ? 0 : min(32, tile >= open_tiles ? a.N - (tile - open_tiles) * 32 : open - tile * 32); };
-    i32x4 k_next[NK];
-    i16x8 v_next[VP];
-    auto fetch = [&](int tile) {   // beyond the last tile: nothing
-        const int valid = keys_of(tile);
-        if (valid <= 0) return;
+    // no node sees a later one: tree keys up to the row tile's last node
+    const int seen_nodes = (min(row0 + RB * 32, a.R) - 1) / a.G + 1;
+    const int open_tiles = (open + 31) / 32, tiles = open_tiles + (seen_nodes + 31) / 32, steps = (tiles + KS - 1) / KS;
+    const int64_t row_b = (int64_t)a.Hkv * ROWB;
+    const int64_t open_at = ((int64_t)b * 2 * kT + L / kT % 2 * kT) * row_b + (int64_t)g * ROWB, tree_at = (int64_t)b * a.N * row_b + (int64_t)g * ROWB;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem + share * 2 * Lay::HALF;
+    auto stage_of = [](int step) { return (step & (Lay::NSTAGE - 1)) * Lay::STAGE; };
+    auto fill = [&](int step) {   // rows beyond the tile's last repeat it: their weights are zero, and their values finite
+        const int tile = min(step * KS + share, tiles - 1);
         const bool in_tree = tile >= open_tiles;
-        const int64_t k0 = (in_tree ? tile - open_tiles : tile) * 32;
-        const uint16_t* const kp = (in_tree ? k_tree : k_open) + (k0 + min(n, valid - 1)) * row_e + 8 * half;
-        const uint16_t* const vp = (in_tree ? v_tree : v_open) + k0 * row_e;
+        const int k0 = (in_tree ? tile - open_tiles : tile) * 32, last = (in_tree ? a.N : open) - 1 - k0;
+        const unsigned char* const kb = static_cast<const unsigned char*>(in_tree ? a.k_tree : a.k_tail) + (in_tree ? tree_at : open_at) + k0 * row_b;
+        const unsigned char* const vb = static_cast<const unsigned char*>(in_tree ? a.v_tree : a.v_tail) + (in_tree ? tree_at : open_at) + k0 * row_b;
+        const uint32_t to = lds0 + stage_of(step);
 #pragma unroll
-        for (int k = 0; k < NK; ++k) k_next[k] = *reinterpret_cast<const i32x4*>(kp + 16 * k);
-#pragma unroll
-        for (int u = 0; u < VP; ++u) {
-            const int p = (rb + u * RB) * 64 + lane, key = p % 32, d = p / 32 * 8;
-            v_next[u] = i16x8{};   // keys beyond the last are zeros (0 * what lies there need not be 0)
-            if (key < valid && p < PIECES) v_next[u] = *reinterpret_cast<const i16x8*>(vp + key * row_e + d);
+        for (int c = 0; c < Lay::LOADS; ++c) {
+            const bool is_v = Lay::CHUNKS % RB == 0 ? c >= Lay::LOADS / 2 : rb >= Lay::CHUNKS;
+            const int chunk = Lay::CHUNKS % RB == 0 ? c % std::max(Lay::LOADS / 2, 1) * RB + rb : rb % Lay::CHUNKS;
+            const int r = chunk * RPI + lane / SLOTS, slot = lane % SLOTS;
+            const int at = is_v ? slot ^ ((r & (NDB - 1)) << 2) : slot ^ (r & (SLOTS - 1));
+            dma_load16_flat<false>((is_v ? vb : kb) + min(r, last) * row_b + 16 * at, to + (is_v ? Lay::HALF : 0) + chunk * 1024);
         }
     };
+    __syncthreads();   // the blocks' tiles are read
+    fill(0);
+    const int row = min(row0 + rb * 32 + n, a.R - 1);
+    const int node = row / a.G, h = g * a.G + row % a.G;
     i32x4 q[NK];
     const uint16_t* const qp = static_cast<const uint16_t*>(a.q) + (((int64_t)b * a.N + node) * a.Hq + h) * DH + 8 * half;
 #pragma unroll
     for (int k = 0; k < NK; ++k) q[k] = *reinterpret_cast<const i32x4*>(qp + 16 * k);
-    __syncthreads();   // the tiles of the blocks are read
-    for (int j = tid; j < a.N; j += NW * 64) parent_s[j] = a.parent_idx[(int64_t)b * a.N + j];
+    for (int j = tid; j < seen_nodes; j += NW * 64) parent_s[j] = a.parent_idx[(int64_t)b * a.N + j];
     if (share == 0)
         for (int w = lane; w < 32 * words; w += 64) mask_s[w] = 0;
     __syncthreads();
@@ -240,28 +257,28 @@ __device__ __forceinline__ void own_keys(const Block8Args& a, unsigned char* sme
             if (p < 0 || p >= j) break;
             j = p;
         }
+    // K operand of step k: row n, slot 2k + half; V: the transpose read gives a lane four keys of one dimension
+    const int k_lane = n * ROWB, k_xor = n & (SLOTS - 1);
+    const int v_row = 4 * half + ((lane & 15) >> 2);
+    const int v_lane = v_row * ROWB + 8 * (lane & 3), v_pair = (lane >> 4) & 1, v_xor = (v_row & (NDB - 1)) << 1;
     const float scale = a.scale * kLog2e;
-    for (int it = 0; it < tiles; it += KS) {
-        const int tile = it + share;
-        const bool in_tree = tile >= open_tiles;
-        const int valid = keys_of(tile);
-        fetch(tile);
-        if (it > 0) __syncthreads();   // the previous V^T is read
-        if (valid > 0)
-#pragma unroll
-            for (int u = 0; u < VP; ++u) {
-                const int p = (rb + u * RB) * 64 + lane, at = p % 32, d = p / 32 * 8;
-                if (p >= PIECES) break;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) vt[(d + e) * Lay::VROW + at] = (uint16_t)v_next[u][e];
-            }
+    for (int i = 1; i < Lay::AHEAD; ++i) fill(i);
+    for (int step = 0; step < steps; ++step) {
+        dma_wait_keep<(Lay::AHEAD - 1) * Lay::LOADS>();
         __syncthreads();
-        if (valid <= 0) continue;   // (nor any later tile)
+        fill(step + Lay::AHEAD);
+        const int tile = step * KS + share;
+        if (tile >= tiles || !active) continue;
+        const bool in_tree = tile >= open_tiles;
+        const unsigned char* const kt = smem + stage_of(step) + share * 2 * Lay::HALF;
+        const unsigned char* const vt = kt + Lay::HALF;
         f32x16 s = {};
 #pragma unroll
         for (int k = 0; k < NK; ++k)
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k_next[k]), __builtin_bit_cast(bf16x8, q[k]), s, 0, 0, 0);
-        const uint32_t seen = in_tree ? mask_s[(tile - open_tiles) * 32 + n] : valid == 32 ? 0xffffffffu : (1u << valid) - 1u;
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kt + k_lane + 16 * ((2 * k + half) ^ k_xor)),
+                                                        __builtin_bit_cast(bf16x8, q[k]), s, 0, 0, 0);
+        const int valid = open - tile * 32;
+        const uint32_t seen = in_tree ? mask_s[(tile - open_tiles) * 32 + n] : valid >= 32 ? 0xffffffffu : (1u << valid) - 1u;
         float top = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -289,31 +306,31 @@ __device__ __forceinline__ void own_keys(const Block8Args& a, unsigned char* sme
             for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(p[8 * k + 2 * e], p[8 * k + 2 * e + 1]);
 #pragma unroll
             for (int d = 0; d < NDB; ++d) {
-                const uint16_t* const v = vt + (32 * d + n) * Lay::VROW + 16 * k + 4 * half;
-                const u32x2 y = *reinterpret_cast<const u32x2*>(v), z = *reinterpret_cast<const u32x2*>(v + 8);
-                const u32x4 operand = {y[0], y[1], z[0], z[1]};
+                const unsigned char* const v = vt + v_lane + 16 * k * ROWB + 32 * ((2 * d + v_pair) ^ v_xor);
+                const i16x8 operand = __builtin_shufflevector(lds_read_tr16(v), lds_read_tr16(v + 8 * ROWB), 0, 1, 2, 3, 4, 5, 6, 7);
                 x.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, operand), __builtin_bit_cast(bf16x8, w), x.o[d], 0, 0, 0);
             }
         }
     }
+    dma_wait_keep<0>();
 }
 
 // Blocks t0 .. t1 - 1 of one stream.
-template <int DH, int NW, int RB>
-__device__ __forceinline__ void cache_blocks(const Block8Args& a, unsigned char* smem, Rows<DH>& x, int b, int g, int row0, int t0, int t1) {
+template <int DH, int NW, int RB, bool NT>
+__device__ __forceinline__ void cache_blocks(unsigned char* smem, Rows<DH>& x, int b, int g, int row0, int t0, int t1) {
+    Args& a = arguments();
     using Lay = Layout<DH, NW, RB>;
     constexpr int KS = Lay::KS, J = DH / 64, NDB = DH / 32;
-    constexpr int CH = Lay::HALF / 1024;           // chunks of a tile of K
-    constexpr int LOADS = 2 * CH / RB;             // direct loads of a wavefront per tile, of K and V
-    constexpr int AHEAD = Lay::NSTAGE - 1;
-    const int tid = threadIdx.x, lane = tid & 63;
+    constexpr int CH = Lay::CHUNKS, LOADS = Lay::LOADS, AHEAD = Lay::AHEAD;
+    const int tid = thread_index(), lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, half = lane >> 5;
     const int rb = wave % RB, share = wave / RB;
 
     const int64_t stream = ((int64_t)b * a.Hkv + g) * a.nblk;
     const int tiles = t1 - t0, steps = (tiles + KS - 1) / KS;
-    const int mine = (tiles - share + KS - 1) / KS;   // this share's tiles: share, share + KS, ..
+    const bool active = row0 + rb * 32 < a.R;
+    const int mine = active ? (tiles - share + KS - 1) / KS : 0;   // this share's tiles: share, share + KS, ..
     const unsigned char* const kc = static_cast<const unsigned char*>(a.k_codes) + stream * kT * DH;
     const unsigned char* const vc = static_cast<const unsigned char*>(a.v_codes) + stream * kT * DH;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem + share * 2 * Lay::HALF;
@@ -328,16 +345,22 @@ __device__ __forceinline__ void cache_blocks(const Block8Args& a, unsigned char*
         for (int c = 0; c < LOADS; ++c) {
             if constexpr (CH % RB == 0) {
                 const int chunk = (c % (LOADS / 2)) * RB + rb;
-                if (c < LOADS / 2) dma_load16<false, 0>(kb + chunk * 1024, (uint32_t)lane * 16, to_k + chunk * 1024);
-                else dma_load16<false, 0>(vb + chunk * 1024, (uint32_t)lane * 16, to_v + chunk * 1024);
+                if (c < LOADS / 2) dma_load16<NT, 0>(kb + chunk * 1024, (uint32_t)lane * 16, to_k + chunk * 1024);
+                else dma_load16<NT, 0>(vb + chunk * 1024, (uint32_t)lane * 16, to_v + chunk * 1024);
             } else {   // twice as many wavefronts as chunks: K's, then V's
                 const int chunk = rb % CH;
-                dma_load16<false, 0>((rb < CH ? kb : vb) + chunk * 1024, (uint32_t)lane * 16, (rb < CH ? to_k : to_v) + chunk * 1024);
+                dma_load16<NT, 0>((rb < CH ? kb : vb) + chunk * 1024, (uint32_t)lane * 16, (rb < CH ? to_k : to_v) + chunk * 1024);
             }
         }
     };
 
-    // Q: this lane's row, dimensions 64 j + 32 half .. + 31
+#pragma unroll
+    for (int c = 0; c < LOADS; ++c)
+        if (c * RB + rb < CH)
+            dma_load16<NT, 0>(kc + (int64_t)tile_of(0) * Lay::HALF + (c * RB + rb) * 1024, (uint32_t)lane * 16, lds0 + (c * RB + rb) * 1024);
+    fill(1, -1);
+
+    // Q: this lane's row, dimensions 64 j + 32 half .. + 31.  (Its loads come behind the first fills, and so does the wait for them.)
     const int row = min(row0 + rb * 32 + n, a.R - 1);
     const int node = row / a.G, h = g * a.G + row % a.G;
     const uint16_t* const qp = static_cast<const uint16_t*>(a.q) + (((int64_t)b * a.N + node) * a.Hq + h) * DH + 32 * half;
@@ -385,13 +408,8 @@ __device__ __forceinline__ void cache_blocks(const Block8Args& a, unsigned char*
         else __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
     };
 
-    dma_wait_keep<0>();
-#pragma unroll
-    for (int c = 0; c < LOADS; ++c)
-        if (c * RB + rb < CH)
-            dma_load16<false, 0>(kc + (int64_t)tile_of(0) * Lay::HALF + (c * RB + rb) * 1024, (uint32_t)lane * 16, lds0 + (c * RB + rb) * 1024);
-    for (int i = 0; i < AHEAD; ++i) fill(i + 1, i - 1);
-    dma_wait_keep<AHEAD * LOADS>();
+    for (int i = 1; i < AHEAD; ++i) fill(i + 1, i - 1);
+    dma_wait_keep<(AHEAD - 1) * LOADS>();
     meet();
     const float scale = a.scale * kLog2e;
     auto advance = [&](int step, f32x16 (&s)[2], f32x16 (&next)[2], const Weights& old, Weights& w) {
@@ -400,6 +418,7 @@ __device__ __forceinline__ void cache_blocks(const Block8Args& a, unsigned char*
         dma_wait_keep<(AHEAD - 1) * LOADS>();
         meet();
         fill(step + 1 + AHEAD, step - 1 + AHEAD);
+        if (!active) return;
         float top = -INFINITY;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
@@ -497,19 +516,12 @@ __device__ __forceinline__ void cache_blocks(const Block8Args& a, unsigned char*
     }
 }
 
-// The batch laid end to end, in units of a block's time: of each sequence kLead empty units (what a segment costs beside its keys), its
-// full blocks, and a.own units for its own keys.  Run r of a.runs has the units r * per .. (r + 1) * per - 1 and the own keys whose middle
+// The batch laid end to end, in units of a block's time: of each sequence a.lead empty units (what a segment costs beside its keys), its
+// full blocks, and a.own units for its own keys.  Run r of `runs` has the units r * per .. (r + 1) * per - 1 and the own keys whose middle
 // lies there, or in the run after the sequence's last block where that is further on.
-template <int DH, int NW, int RB>
-__global__ __launch_bounds__(NW * 64, NW / 4) void attn_block8_kernel(Block8Args a) {
-    extern __shared__ __align__(16) unsigned char smem[];
+template <int DH, int NW, int RB, bool NT>
+__device__ __forceinline__ void serve(const Block8Args& a, unsigned char* smem, int g, int run, int runs, int row0, int32_t* seq_splits) {
     float* const stat = reinterpret_cast<float*>(smem + a.stat_at);
-    // a stream's row tiles share an XCD, and so an L2: workgroup -> XCD is round robin
-    const int xcd = blockIdx.x % 8, rest = blockIdx.x / 8;
-    const int row0 = rest % a.row_tiles * RB * 32;
-    const int stream = rest / a.row_tiles * 8 + xcd;
-    if (stream >= a.runs * a.Hkv) return;
-    const int run = stream / a.Hkv, g = stream % a.Hkv;
     const int lane = threadIdx.x & 63;
     auto length = [&](int b) {
         const int L = b < a.B ? a.seq_lens[b] : 0;
@@ -519,7 +531,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_block8_kernel(Block8Args
     int total = wave_sum_i32(L / kT);
     for (int b0 = 64; b0 < a.B; b0 += 64) total += wave_sum_i32(length(b0 + lane) / kT);
     total += a.B * (a.lead + a.own);
-    const int per = (total + a.runs - 1) / a.runs;
+    const int per = (total + runs - 1) / runs;
     int before = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
         if (b0 > 0) L = length(b0 + lane);
@@ -527,66 +539,166 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_block8_kernel(Block8Args
         const int sums = wave_prefix_i32(units, lane);
         const int first = before + sums - units + a.lead;            // unit of the first block
         before += __builtin_amdgcn_readlane(sums, 63);
-        int first_run = first / per, own_run = (first + blocks + a.own / 2) / per;
-        if (blocks > 0) own_run = min(own_run, (first + blocks - 1) / per + 1);
-        else first_run = own_run;
-        const int splits = own_run - first_run + 1;
-        if (run == 0 && g == 0 && row0 == 0 && threadIdx.x < 64 && units > 0) a.seq_splits[b0 + lane] = splits > 1 ? splits : 0;
+        // the run of a sequence's first work and that of its own keys
+        auto runs_of = [&](int at, int nb, int& first_run, int& own_run) {
+            own_run = (at + nb + a.own / 2) / per;
+            first_run = nb > 0 ? at / per : own_run;
+            if (nb > 0) own_run = min(own_run, (at + nb - 1) / per + 1);
+        };
+        int first_run, own_run;
+        runs_of(first, blocks, first_run, own_run);
+        if (seq_splits && threadIdx.x < 64 && units > 0) seq_splits[b0 + lane] = own_run > first_run ? own_run - first_run + 1 : 0;
         uint64_t todo = __ballot(units > 0 && run >= first_run && run <= own_run);
         while (todo) {
             const int i = __builtin_ctzll(todo);
             todo &= todo - 1;
-            const int at = __builtin_amdgcn_readlane(first, i), nb = __builtin_amdgcn_readlane(blocks, i);
+            const int at = __builtin_amdgcn_readlane(first, i), length = __builtin_amdgcn_readlane(L, i), nb = length / kT;
+            int from, to;
+            runs_of(at, nb, from, to);
             const int t0 = max(run * per - at, 0), t1 = min((run + 1) * per - at, nb);
-            const bool own = run == __builtin_amdgcn_readlane(own_run, i);
-            const int split = run - __builtin_amdgcn_readlane(first_run, i);
             Rows<DH> x;
             x.clear();
-            if (t0 < t1) cache_blocks<DH, NW, RB>(a, smem, x, b0 + i, g, row0, t0, t1);
-            if (own) own_keys<DH, NW, RB>(a, smem, x, b0 + i, g, row0, __builtin_amdgcn_readlane(L, i));
-            write_rows<DH, NW, RB>(a, smem, stat, x, b0 + i, g, row0, __builtin_amdgcn_readlane(splits, i) > 1 ? split : -1);
+            if (t0 < t1) cache_blocks<DH, NW, RB, NT>(smem, x, b0 + i, g, row0, t0, t1);
+            if (run == to) own_keys<DH, NW, RB, NT>(smem, x, b0 + i, g, row0, length);
+            write_rows<DH, NW, RB>(smem, stat, x, b0 + i, g, row0, to > from ? run - from : -1);
         }
     }
 }
 
-template <int DH, int NW, int RB>
-hipError_t raise(int) {
-    return hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_block8_kernel<DH, NW, RB>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                               (int)kAttnMfmaMaxSmem);
+// RB row blocks to a workgroup; the row blocks beyond the last whole tile of eight have workgroups of REM row blocks and runs of their own.
+template <int DH, int NW, int RB, int REM, bool NT>
+__global__ __launch_bounds__(NW * 64, NW / 4) void attn_block8_kernel(Block8Args a) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    // a stream's row tiles share an XCD, and so an L2: workgroup -> XCD is round robin
+    const int id = blockIdx.x;
+    if (REM == 0 || id < a.main_groups) {
+        const int xcd = id % 8, rest = id / 8;
+        const int tile = rest % a.row_tiles, stream = rest / a.row_tiles * 8 + xcd;
+        if (stream >= a.runs * a.Hkv) return;
+        const int run = stream / a.Hkv, g = stream % a.Hkv;
+        serve<DH, NW, RB, NT>(a, smem, g, run, a.runs, tile * RB * 32, stream == 0 && tile == 0 ? a.seq_splits : nullptr);
+    } else if constexpr (REM > 0) {
+        const int stream = id - a.main_groups, run = stream / a.Hkv, g = stream % a.Hkv;
+        serve<DH, NW, REM, NT>(a, smem, g, run, a.rem_runs, a.row_tiles * RB * 32, stream == 0 ? a.seq_splits + a.B : nullptr);
+    }
 }
 
-template <int DH, int NW, int RB>
+// Merge of a row's partials: m* = max m_s, l* = sum l_s 2^(m_s - m*), O = sum O~_s c_s 2^(m_s - m*) / l*.  DH / 8 lanes to a row, and
+// GRP such groups that take every GRP-th split each; eight partials of a group are requested at once.
+template <int DH, int GRP>
+__global__ __launch_bounds__(256) void block8_merge_kernel(Block8Args a) {
+    constexpr int LPR = DH / 8, LANES = LPR * GRP, AT_ONCE = 8;
+    const int b = blockIdx.y;
+    const int row = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, rows = a.N * a.Hq;
+    if (row >= rows) return;   // (a row's lanes go together)
+    const int col = threadIdx.x % LPR, grp = threadIdx.x % LANES / LPR;
+    const int local = row / a.Hq * a.G + row % a.Hq % a.G;
+    const int splits = a.seq_splits[local < a.main_rows ? b : a.B + b];
+    if (splits == 0) return;   // final already
+    const int64_t r = (int64_t)b * rows + row;
+    const f16x8* const po = static_cast<const f16x8*>(a.part_o) + r * LPR + col;
+    float m = -INFINITY, l = 0.f, acc[8] = {};
+    for (int s0 = grp; s0 < splits; s0 += GRP * AT_ONCE) {
+        float3 rec[AT_ONCE];
+        f16x8 raw[AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const int64_t s = min(s0 + u * GRP, splits - 1);
+            rec[u] = a.part_rec[s * a.rows_total + r];
+            raw[u] = po[s * a.rows_total * LPR];
+        }
+        float top = m;
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) top = fmaxf(top, rec[u].x);
+        const float fix = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        l *= fix;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] *= fix;
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const bool there = s0 + u * GRP < splits && rec[u].x != -INFINITY;
+            const float w = there ? __builtin_amdgcn_exp2f(rec[u].x - top) : 0.f;
+            l = fmaf(rec[u].y, w, l);
+            const float wc = w * rec[u].z;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] = fmaf((float)raw[u][e], wc, acc[e]);
+        }
+        m = top;
+    }
+#pragma unroll
+    for (int o = LPR; o < LANES; o <<= 1) {
+        const float m2 = __shfl_xor(m, o), top = fmaxf(m, m2);
+        const float mine = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top), other = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m2 - top);
+        l = l * mine + __shfl_xor(l, o) * other;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = acc[e] * mine + __shfl_xor(acc[e], o) * other;
+        m = top;
+    }
+    if (grp > 0) return;
+    const float inv = 1.f / l;
+    u32x4 y;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) y[k] = pack_bf16x2(acc[2 * k] * inv, acc[2 * k + 1] * inv);
+    static_cast<u32x4*>(a.out)[r * LPR + col] = y;
+    if (a.lse && col == 0) a.lse[r] = m * kLn2 + logf(l);
+}
+
+template <int DH, int NW, int RB, int REM>
+hipError_t raise() {
+    hipError_t e = hipSuccess;
+    for (const void* f : {reinterpret_cast<const void*>(&attn_block8_kernel<DH, NW, RB, REM, false>),
+                          reinterpret_cast<const void*>(&attn_block8_kernel<DH, NW, RB, REM, true>)})
+        if (const hipError_t x = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kAttnMfmaMaxSmem); x != hipSuccess) e = x;
+    return e;
+}
+
+template <int DH, int NW, int RB, int REM>
 hipError_t launch(Block8Args a, hipStream_t st) {
-    const size_t smem = Layout<DH, NW, RB>::smem(a.N);
+    size_t smem = Layout<DH, NW, RB>::smem(a.N);
+    if constexpr (REM > 0) smem = std::max(smem, Layout<DH, NW, REM>::smem(a.N));
     if (smem > kAttnMfmaMaxSmem) return hipErrorInvalidValue;
-    a.stat_at = (int32_t)(smem - Layout<DH, NW, RB>::STAT);
+    a.stat_at = (int32_t)(smem - NW * 32 * 2 * sizeof(float));
     const int64_t streams = (int64_t)a.runs * a.Hkv;
-    const dim3 grid((unsigned)((streams + 7) / 8 * 8 * a.row_tiles));
-    hipLaunchKernelGGL((attn_block8_kernel<DH, NW, RB>), grid, dim3(NW * 64), smem, st, a);
+    a.main_groups = (int32_t)((streams + 7) / 8 * 8 * a.row_tiles);
+    const dim3 grid((unsigned)(a.main_groups + (REM > 0 ? a.rem_runs * a.Hkv : 0)));
+    // the streaming hint where a workgroup is its stream's only reader
+    if (a.row_tiles == 1 && REM == 0) hipLaunchKernelGGL((attn_block8_kernel<DH, NW, RB, REM, true>), grid, dim3(NW * 64), smem, st, a);
+    else hipLaunchKernelGGL((attn_block8_kernel<DH, NW, RB, REM, false>), grid, dim3(NW * 64), smem, st, a);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess || (a.runs == 1 && (REM == 0 || a.rem_runs == 1))) return e;
+    constexpr int LPR = DH / 8;
+    auto groups = [&](int lanes) { return dim3((unsigned)(((int64_t)a.N * a.Hq * lanes + 255) / 256), (unsigned)a.B); };
+    // few rows: a whole wavefront to each
+    if (a.rows_total <= 4096) hipLaunchKernelGGL((block8_merge_kernel<DH, 64 / LPR>), groups(64), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((block8_merge_kernel<DH, 1>), groups(LPR), dim3(256), 0, st, a);
     return hipGetLastError();
+}
+
+template <int DH>
+hipError_t launch_for(const Block8Args& a, const Block8Plan& p, hipStream_t st) {
+    switch (p.row_blocks * 10 + p.rem_blocks) {
+        case 10: return launch<DH, 4, 1, 0>(a, st);
+        case 20: return launch<DH, 8, 2, 0>(a, st);
+        case 40: return launch<DH, 8, 4, 0>(a, st);
+        case 80: return launch<DH, 8, 8, 0>(a, st);
+        case 82: return launch<DH, 8, 8, 2>(a, st);
+        case 84: return launch<DH, 8, 8, 4>(a, st);
+        default: return hipErrorInvalidValue;
+    }
 }
 
 }  // namespace
 
 hipError_t raise_limits_attn_block8() {
     hipError_t e = hipSuccess;
-    for (hipError_t x : {raise<128, 8, 8>(0), raise<128, 8, 4>(0), raise<128, 8, 2>(0), raise<128, 4, 1>(0), raise<64, 8, 8>(0),
-                         raise<64, 8, 4>(0), raise<64, 8, 2>(0), raise<64, 4, 1>(0)})
+    for (hipError_t x : {raise<128, 4, 1, 0>(), raise<128, 8, 2, 0>(), raise<128, 8, 4, 0>(), raise<128, 8, 8, 0>(), raise<128, 8, 8, 2>(),
+                         raise<128, 8, 8, 4>(), raise<64, 4, 1, 0>(), raise<64, 8, 2, 0>(), raise<64, 8, 4, 0>(), raise<64, 8, 8, 0>(),
+                         raise<64, 8, 8, 2>(), raise<64, 8, 8, 4>()})
         if (x != hipSuccess) e = x;
     return e;
 }
 
 hipError_t launch_attn_block8(const Block8Args& a, const Block8Plan& p, int head_dim, hipStream_t st) {
-    auto go = [&](auto dh) {
-        constexpr int DH = decltype(dh)::value;
-        switch (p.row_blocks) {
-            case 1: return launch<DH, 4, 1>(a, st);
-            case 2: return launch<DH, 8, 2>(a, st);
-            case 4: return launch<DH, 8, 4>(a, st);
-            default: return launch<DH, 8, 8>(a, st);
-        }
-    };
-    return head_dim == 128 ? go(std::integral_constant<int, 128>{}) : go(std::integral_constant<int, 64>{});
+    return head_dim == 128 ? launch_for<128>(a, p, st) : launch_for<64>(a, p, st);
 }
 
 }  // namespace ygg

@@ -272,29 +272,44 @@ static size_t attention_scratch_bytes(const ygg_shape& s) {
     return part_o_bytes(s, p.use_mfma, most) + part_rec_bytes(s, most) + p.seq_splits_bytes;
 }
 
-// Workgroup shape and runs of the attention over the block cache.
+// Workgroup shapes and runs of the attention over the block cache.
 Block8Plan plan_block8(const ygg_shape& s) {
     Block8Plan p{};
-    const int64_t R = (int64_t)s.n_nodes * (s.n_q_heads / s.n_kv_heads);
-    p.row_blocks = R <= 32 ? 1 : R <= 64 ? 2 : R <= 128 ? 4 : 8;
-    p.row_tiles = (int32_t)((R + p.row_blocks * 32 - 1) / (p.row_blocks * 32));
+    const int64_t R = (int64_t)s.n_nodes * (s.n_q_heads / s.n_kv_heads), row_blocks = (R + 31) / 32;
+    p.row_blocks = row_blocks <= 1 ? 1 : row_blocks <= 2 ? 2 : row_blocks <= 4 ? 4 : 8;
+    p.row_tiles = (int32_t)((row_blocks + p.row_blocks - 1) / p.row_blocks);
+    // One to four row blocks beyond whole tiles of eight: a smaller shape, whose wavefronts deal out the tiles of keys instead of idling.
+    if (row_blocks > 8 && row_blocks % 8 >= 1 && row_blocks % 8 <= 4) {
+        p.row_tiles = (int32_t)(row_blocks / 8);
+        p.rem_blocks = row_blocks % 8 <= 2 ? 2 : 4;
+    }
     p.lead = 2;
     p.own = 2 + (s.n_nodes + 31) / 32;
-    // Runs: as many as fill the chip with whole rounds of workgroups (one to a compute unit), and of one to four rounds those that take
-    // least time, a round being the units of a run and a start.
-    const int64_t at_once = std::max(streams_at_once(p.row_tiles), (int64_t)1);
     const int64_t units = (int64_t)s.batch * (s.max_seq_len / YGG_KV_BLOCK + p.lead + p.own);
+    const int64_t most = std::min((int64_t)64, units), Hkv = s.n_kv_heads;
+    // Runs: as many as fill the chip with whole rounds of workgroups (one to a compute unit), and of one to four rounds those that take
+    // least time, a round being the units of a run and a start.  Workgroups beyond the whole tiles share the first round's compute
+    // units: they take rem_blocks / 8 of a run's time per unit.
     int64_t best = 0;
     for (int64_t rounds = 1; rounds <= 4; ++rounds) {
-        const int64_t runs = std::clamp(rounds * at_once / s.n_kv_heads, (int64_t)1, std::min((int64_t)64, units));
-        const int64_t need = (runs * s.n_kv_heads + at_once - 1) / at_once;
+        const int64_t slots = 256 * rounds / Hkv;      // compute units to a kv head, over the rounds
+        int64_t rem = 0, runs = 0;
+        if (p.rem_blocks) {
+            const int64_t all = 8 * p.row_tiles + p.rem_blocks;
+            rem = std::clamp((slots * p.rem_blocks + all - 1) / all, (int64_t)1, most);
+            runs = std::clamp((slots - rem) / p.row_tiles, (int64_t)1, most);
+        } else {
+            runs = std::clamp(rounds * std::max(streams_at_once(p.row_tiles), (int64_t)1) / Hkv, (int64_t)1, most);
+        }
+        const int64_t need = ((runs * p.row_tiles + rem) * Hkv + 255) / 256;
         const int64_t time = need * ((units + runs - 1) / runs + 4);
-        if (rounds == 1 || time < best) { best = time; p.runs = (int32_t)runs; }
-        p.most_runs = (int32_t)runs;
+        if (rounds == 1 || time < best) { best = time; p.runs = (int32_t)runs; p.rem_runs = (int32_t)rem; }
+        p.most_runs = (int32_t)std::max({runs, rem, (int64_t)p.most_runs});
     }
-    p.part_o_bytes = part_o_bytes(s, true, p.runs);
-    p.part_rec_bytes = part_rec_bytes(s, p.runs);
-    p.seq_splits_bytes = align256((size_t)s.batch * sizeof(int32_t));
+    const int32_t nsplit = std::max(p.runs, p.rem_runs);
+    p.part_o_bytes = part_o_bytes(s, true, nsplit);
+    p.part_rec_bytes = part_rec_bytes(s, nsplit);
+    p.seq_splits_bytes = align256(2 * (size_t)s.batch * sizeof(int32_t));
     return p;
 }
 
@@ -604,7 +619,7 @@ int32_t ygg_tree_attention_block8(const ygg_shape* s, const void* q, const ygg_b
     const int64_t rows = (int64_t)s->batch * s->n_nodes * s->n_q_heads;
     const Block8Plan p = plan_block8(*s);
     // the kernels count query rows, workgroups and a batch's blocks with 31 bits
-    if (rows > 0x7fffffffLL || ((int64_t)p.runs + 8) * s->n_kv_heads * p.row_tiles > 0x7fffffffLL ||
+    if (rows > 0x7fffffffLL || ((int64_t)p.runs + p.rem_runs + 8) * s->n_kv_heads * p.row_tiles > 0x7fffffffLL ||
         (int64_t)s->batch * (s->max_seq_len / YGG_KV_BLOCK + p.lead + p.own) > 0x3fffffffLL) return YGG_ERR_UNSUPPORTED;
     if (int32_t rc = check_workspace(workspace, workspace_bytes, p.part_o_bytes + p.part_rec_bytes + p.seq_splits_bytes)) return rc;
     if (int32_t rc = ensure_device_ready()) return rc;
@@ -620,17 +635,10 @@ int32_t ygg_tree_attention_block8(const ygg_shape* s, const void* q, const ygg_b
     a.rows_total = rows;
     a.B = s->batch; a.N = s->n_nodes; a.Hq = s->n_q_heads; a.Hkv = s->n_kv_heads; a.G = a.Hq / a.Hkv; a.R = a.N * a.G;
     a.out = out; a.lse = lse;
-    a.row_tiles = p.row_tiles; a.runs = p.runs; a.lead = p.lead; a.own = p.own; a.max_seq_len = s->max_seq_len; a.scale = s->softmax_scale;
+    a.row_tiles = p.row_tiles; a.runs = p.runs; a.rem_runs = p.rem_runs; a.lead = p.lead; a.own = p.own;
+    a.main_rows = p.row_tiles * p.row_blocks * 32; a.max_seq_len = s->max_seq_len; a.scale = s->softmax_scale;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (launch_attn_block8(a, p, s->head_dim, st) != hipSuccess) return YGG_ERR_LAUNCH;
-    if (p.runs == 1) return YGG_OK;   // every sequence is one segment
-
-    AttnArgs m{};      // the merge of the splits, shared with the other matrix-core kernels
-    m.part_o = a.part_o; m.part_rec = a.part_rec; m.seq_splits = a.seq_splits; m.out = out; m.lse = lse;
-    m.B = a.B; m.N = a.N; m.Hq = a.Hq; m.Hkv = a.Hkv; m.Dh = s->head_dim; m.nsplit = p.runs; m.rows_total = (int32_t)rows;
-    AttnPlan mp{};
-    mp.use_mfma = 1;
-    return launch_attn_combine(m, mp, YGG_BF16, st) == hipSuccess ? YGG_OK : YGG_ERR_LAUNCH;
+    return launch_attn_block8(a, p, s->head_dim, st) == hipSuccess ? YGG_OK : YGG_ERR_LAUNCH;
 }
 
 int32_t ygg_block8_append(const ygg_shape* s, int32_t n_layers, const void* k_new, const void* v_new, int32_t n_rows,

@@ -159,8 +159,9 @@ hipError_t launch_accept(const AcceptArgs& a, hipStream_t st);
 // ---- attention over the 8-bit block cache ----------------------------------------------------------
 struct Block8Plan {
     int32_t row_blocks;   // 32-row blocks to a workgroup: 1, 2, 4 or 8
-    int32_t row_tiles;    // workgroups along the N*G query rows of one kv head
-    int32_t runs;         // equal runs of the batch's keys per (kv head, row tile), one workgroup each, at most 64
+    int32_t row_tiles;    // workgroups of that shape along the N*G query rows of one kv head
+    int32_t rem_blocks;   // 2 or 4: the rows beyond them go to workgroups of that many row blocks; 0: there are none
+    int32_t runs, rem_runs;   // equal runs of the batch's keys per (kv head, row tile), one workgroup each, at most 64
     int32_t most_runs;    // the most that this or a shorter bound on the lengths may take
     int32_t lead, own;    // what a segment costs beside its keys, and a sequence's own keys, in blocks
     size_t part_o_bytes, part_rec_bytes, seq_splits_bytes;
@@ -179,12 +180,14 @@ struct Block8Args {
     const int32_t* parent_idx;
     void* part_o;          // as in AttnArgs, matrix-core format
     float3* part_rec;
-    int32_t* seq_splits;   // as in AttnArgs
+    int32_t* seq_splits;   // [2][B]: partials of a sequence's rows (0: the rows are final), of whole row tiles and of those beyond
     void* out;
     float* lse;
     int64_t nblk, rows_total;
     int32_t B, N, Hq, Hkv, G, R;   // R = N * G rows share a stream
-    int32_t row_tiles, runs, lead, own, max_seq_len;
+    int32_t row_tiles, runs, rem_runs, lead, own, max_seq_len;
+    int32_t main_rows;             // rows of a kv head in whole row tiles
+    int32_t main_groups;           // workgroups of these
     int32_t stat_at;               // bytes of shared memory in front of the rows' statistics
     float scale;
 };
