@@ -321,7 +321,7 @@ __device__ __forceinline__ void cache_blocks(unsigned char* smem, Rows<DH>& x, i
     Args& a = arguments();
     using Lay = Layout<DH, NW, RB>;
     constexpr int KS = Lay::KS, J = DH / 64, NDB = DH / 32;
-    constexpr int CH = Lay::CHUNKS, LOADS = Lay::LOADS, AHEAD = Lay::AHEAD;
+    constexpr int CH = Lay::CHUNKS, LOADS = Lay::LOADS;
     const int tid = thread_index(), lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, half = lane >> 5;
@@ -408,17 +408,25 @@ __device__ __forceinline__ void cache_blocks(unsigned char* smem, Rows<DH>& x, i
         else __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
     };
 
-    for (int i = 1; i < AHEAD; ++i) fill(i + 1, i - 1);
-    dma_wait_keep<(AHEAD - 1) * LOADS>();
+    // With four stages the wavefronts meet every other step only, and two tiles are requested there: they may then be apart by a step, and
+    // the two of a SIMD less often want the same pipe at once.
+    constexpr bool PAIRS = Lay::NSTAGE == 4;
+    if constexpr (PAIRS) fill(2, 0);
+    dma_wait_keep<PAIRS ? LOADS : 0>();
     meet();
     const float scale = a.scale * kLog2e;
+    const float *const ksp = a.k_scale + stream, *const vsp = a.v_scale + stream;
+    float ks_next = uniform_load(ksp + tile_of(0)), vs_next = uniform_load(vsp + tile_of(0));
     auto advance = [&](int step, f32x16 (&s)[2], f32x16 (&next)[2], const Weights& old, Weights& w) {
-        const int t = tile_of(step);
-        const float ks = uniform_load(a.k_scale + stream + t), vs = uniform_load(a.v_scale + stream + t);
-        dma_wait_keep<(AHEAD - 1) * LOADS>();
-        meet();
-        fill(step + 1 + AHEAD, step - 1 + AHEAD);
+        if constexpr (!PAIRS) {
+            dma_wait_keep<0>();
+            meet();
+            fill(step + 2, step);
+        }
         if (!active) return;
+        const float ks = ks_next, vs = vs_next;   // requested a step ago
+        ks_next = uniform_load(ksp + tile_of(step + 1));
+        vs_next = uniform_load(vsp + tile_of(step + 1));
         float top = -INFINITY;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
@@ -477,7 +485,7 @@ __device__ __forceinline__ void cache_blocks(unsigned char* smem, Rows<DH>& x, i
             op = after;
             __builtin_amdgcn_sched_barrier(0);
         });
-        x.l = fmaf(sum, ldexpf(1.f / significand, max(w.c - x.ref, -127)), x.l);
+        x.l = fmaf(sum, ldexpf(__builtin_amdgcn_rcpf(significand), max(w.c - x.ref, -127)), x.l);
         // the products stay in this step too, and are not moved behind the next one's branch
 #pragma unroll
         for (int u = 0; u < 2; ++u) asm volatile("" : "+v"(next[u]));
@@ -501,6 +509,12 @@ __device__ __forceinline__ void cache_blocks(unsigned char* smem, Rows<DH>& x, i
     }
     int step = 0;
     for (; step < steps; step += 2) {
+        if constexpr (PAIRS) {
+            dma_wait_keep<0>();
+            meet();
+            fill(step + 3, step + 1);
+            fill(step + 4, step + 2);
+        }
         advance(step, s0, s1, w1, w0);
         advance(step + 1, s1, s0, w0, w1);
     }
