@@ -42,8 +42,7 @@ struct Layout {
     static constexpr int CHUNKS = HALF / 1024;            // a direct load of a wavefront brings 1024 bytes
     static constexpr int LOADS = 2 * CHUNKS / RB;         // direct loads of a wavefront per tile
     static constexpr int STAGE = KS * 2 * HALF;           // [share][K, V]
-    static constexpr int NSTAGE = STAGE >= 65536 ? 2 : 4;
-    static constexpr int AHEAD = NSTAGE - 1;              // tiles in flight
+    static constexpr int NSTAGE = 2;
     static constexpr int OROW = DH + 4;                   // floats of a row of O~ in LDS
     static constexpr int MERGE = NW * 32 * OROW * 4;      // in the tiles' place
     static constexpr int STAT = NW * 32 * 2 * 4;          // (reference, sum) of every wavefront's rows, behind everything else
@@ -198,10 +197,11 @@ __device__ __forceinline__ void write_rows(unsigned char* smem, float* stat, Row
     __syncthreads();   // before the next segment's tiles
 }
 
-// The open block's rows and the tree's keys under the ancestor mask, 32 to a tile.  Tiles come in by direct loads, 16-byte slots permuted
+// The open block's rows and the tree's keys under the ancestor mask, 32 to a tile: units 0 and 1 are the open block's, 2 + k the tree's
+// k-th; u0 .. u1 - 1 of them.  Tiles come in by direct loads, 16-byte slots permuted
 // within a row so that operand reads meet no bank twice: K slot ^ row, V slot ^ 4 (row % (DH / 32)).
 template <int DH, int NW, int RB, bool NT>
-__device__ __forceinline__ void own_keys(unsigned char* smem, Rows<DH>& x, int b, int g, int row0, int L) {
+__device__ __forceinline__ void own_keys(unsigned char* smem, Rows<DH>& x, int b, int g, int row0, int L, int u0, int u1) {
     Args& a = arguments();
     using Lay = Layout<DH, NW, RB>;
     constexpr int KS = Lay::KS, NK = DH / 16, NDB = DH / 32, ROWB = 2 * DH, SLOTS = ROWB / 16, RPI = 1024 / ROWB;
@@ -217,15 +217,18 @@ __device__ __forceinline__ void own_keys(unsigned char* smem, Rows<DH>& x, int b
 
     // no node sees a later one: tree keys up to the row tile's last node
     const int seen_nodes = (min(row0 + RB * 32, a.R) - 1) / a.G + 1;
-    const int open_tiles = (open + 31) / 32, tiles = open_tiles + (seen_nodes + 31) / 32, steps = (tiles + KS - 1) / KS;
+    const int open0 = min(u0, (open + 31) / 32), n_open = min(u1, (open + 31) / 32) - open0;
+    const int tree0 = max(u0 - 2, 0), n_tree = max(min(u1 - 2, (seen_nodes + 31) / 32) - tree0, 0);
+    const int tiles = n_open + n_tree, steps = (tiles + KS - 1) / KS;
+    if (tiles == 0) return;
     const int64_t row_b = (int64_t)a.Hkv * ROWB;
     const int64_t open_at = ((int64_t)b * 2 * kT + L / kT % 2 * kT) * row_b + (int64_t)g * ROWB, tree_at = (int64_t)b * a.N * row_b + (int64_t)g * ROWB;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem + share * 2 * Lay::HALF;
     auto stage_of = [](int step) { return (step & (Lay::NSTAGE - 1)) * Lay::STAGE; };
     auto fill = [&](int step) {   // rows beyond the tile's last repeat it: their weights are zero, and their values finite
         const int tile = min(step * KS + share, tiles - 1);
-        const bool in_tree = tile >= open_tiles;
-        const int k0 = (in_tree ? tile - open_tiles : tile) * 32, last = (in_tree ? a.N : open) - 1 - k0;
+        const bool in_tree = tile >= n_open;
+        const int k0 = (in_tree ? tree0 + tile - n_open : open0 + tile) * 32, last = (in_tree ? a.N : open) - 1 - k0;
         const unsigned char* const kb = static_cast<const unsigned char*>(in_tree ? a.k_tree : a.k_tail) + (in_tree ? tree_at : open_at) + k0 * row_b;
         const unsigned char* const vb = static_cast<const unsigned char*>(in_tree ? a.v_tree : a.v_tail) + (in_tree ? tree_at : open_at) + k0 * row_b;
         const uint32_t to = lds0 + stage_of(step);
@@ -262,14 +265,13 @@ __device__ __forceinline__ void own_keys(unsigned char* smem, Rows<DH>& x, int b
     const int v_row = 4 * half + ((lane & 15) >> 2);
     const int v_lane = v_row * ROWB + 8 * (lane & 3), v_pair = (lane >> 4) & 1, v_xor = (v_row & (NDB - 1)) << 1;
     const float scale = a.scale * kLog2e;
-    for (int i = 1; i < Lay::AHEAD; ++i) fill(i);
     for (int step = 0; step < steps; ++step) {
-        dma_wait_keep<(Lay::AHEAD - 1) * Lay::LOADS>();
+        dma_wait_keep<0>();
         __syncthreads();
-        fill(step + Lay::AHEAD);
+        fill(step + 1);
         const int tile = step * KS + share;
         if (tile >= tiles || !active) continue;
-        const bool in_tree = tile >= open_tiles;
+        const bool in_tree = tile >= n_open;
         const unsigned char* const kt = smem + stage_of(step) + share * 2 * Lay::HALF;
         const unsigned char* const vt = kt + Lay::HALF;
         f32x16 s = {};
@@ -277,8 +279,8 @@ __device__ __forceinline__ void own_keys(unsigned char* smem, Rows<DH>& x, int b
         for (int k = 0; k < NK; ++k)
             s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kt + k_lane + 16 * ((2 * k + half) ^ k_xor)),
                                                         __builtin_bit_cast(bf16x8, q[k]), s, 0, 0, 0);
-        const int valid = open - tile * 32;
-        const uint32_t seen = in_tree ? mask_s[(tile - open_tiles) * 32 + n] : valid >= 32 ? 0xffffffffu : (1u << valid) - 1u;
+        const int valid = open - (open0 + tile) * 32;
+        const uint32_t seen = in_tree ? mask_s[(tree0 + tile - n_open) * 32 + n] : valid >= 32 ? 0xffffffffu : (1u << valid) - 1u;
         float top = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -408,21 +410,15 @@ __device__ __forceinline__ void cache_blocks(unsigned char* smem, Rows<DH>& x, i
         else __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
     };
 
-    // With four stages the wavefronts meet every other step only, and two tiles are requested there: they may then be apart by a step, and
-    // the two of a SIMD less often want the same pipe at once.
-    constexpr bool PAIRS = Lay::NSTAGE == 4;
-    if constexpr (PAIRS) fill(2, 0);
-    dma_wait_keep<PAIRS ? LOADS : 0>();
+    dma_wait_keep<0>();
     meet();
     const float scale = a.scale * kLog2e;
     const float *const ksp = a.k_scale + stream, *const vsp = a.v_scale + stream;
     float ks_next = uniform_load(ksp + tile_of(0)), vs_next = uniform_load(vsp + tile_of(0));
     auto advance = [&](int step, f32x16 (&s)[2], f32x16 (&next)[2], const Weights& old, Weights& w) {
-        if constexpr (!PAIRS) {
-            dma_wait_keep<0>();
-            meet();
-            fill(step + 2, step);
-        }
+        dma_wait_keep<0>();
+        meet();
+        fill(step + 2, step);
         if (!active) return;
         const float ks = ks_next, vs = vs_next;   // requested a step ago
         ks_next = uniform_load(ksp + tile_of(step + 1));
@@ -509,12 +505,6 @@ __device__ __forceinline__ void cache_blocks(unsigned char* smem, Rows<DH>& x, i
     }
     int step = 0;
     for (; step < steps; step += 2) {
-        if constexpr (PAIRS) {
-            dma_wait_keep<0>();
-            meet();
-            fill(step + 3, step + 1);
-            fill(step + 4, step + 2);
-        }
         advance(step, s0, s1, w1, w0);
         advance(step + 1, s1, s0, w0, w1);
     }
@@ -531,8 +521,7 @@ __device__ __forceinline__ void cache_blocks(unsigned char* smem, Rows<DH>& x, i
 }
 
 // The batch laid end to end, in units of a block's time: of each sequence a.lead empty units (what a segment costs beside its keys), its
-// full blocks, and a.own units for its own keys.  Run r of `runs` has the units r * per .. (r + 1) * per - 1 and the own keys whose middle
-// lies there, or in the run after the sequence's last block where that is further on.
+// full blocks, and a.own units for the tiles of its own keys.  Run r of `runs` has the units r * per .. (r + 1) * per - 1.
 template <int DH, int NW, int RB, bool NT>
 __device__ __forceinline__ void serve(const Block8Args& a, unsigned char* smem, int g, int run, int runs, int row0, int32_t* seq_splits) {
     float* const stat = reinterpret_cast<float*>(smem + a.stat_at);
@@ -553,27 +542,19 @@ __device__ __forceinline__ void serve(const Block8Args& a, unsigned char* smem, 
         const int sums = wave_prefix_i32(units, lane);
         const int first = before + sums - units + a.lead;            // unit of the first block
         before += __builtin_amdgcn_readlane(sums, 63);
-        // the run of a sequence's first work and that of its own keys
-        auto runs_of = [&](int at, int nb, int& first_run, int& own_run) {
-            own_run = (at + nb + a.own / 2) / per;
-            first_run = nb > 0 ? at / per : own_run;
-            if (nb > 0) own_run = min(own_run, (at + nb - 1) / per + 1);
-        };
-        int first_run, own_run;
-        runs_of(first, blocks, first_run, own_run);
-        if (seq_splits && threadIdx.x < 64 && units > 0) seq_splits[b0 + lane] = own_run > first_run ? own_run - first_run + 1 : 0;
-        uint64_t todo = __ballot(units > 0 && run >= first_run && run <= own_run);
+        const int first_run = first / per, last_run = (first + blocks + a.own - 1) / per;
+        if (seq_splits && threadIdx.x < 64 && units > 0) seq_splits[b0 + lane] = last_run > first_run ? last_run - first_run + 1 : 0;
+        uint64_t todo = __ballot(units > 0 && run >= first_run && run <= last_run);
         while (todo) {
             const int i = __builtin_ctzll(todo);
             todo &= todo - 1;
             const int at = __builtin_amdgcn_readlane(first, i), length = __builtin_amdgcn_readlane(L, i), nb = length / kT;
-            int from, to;
-            runs_of(at, nb, from, to);
-            const int t0 = max(run * per - at, 0), t1 = min((run + 1) * per - at, nb);
+            const int from = at / per, to = (at + nb + a.own - 1) / per;
+            const int lo = max(run * per - at, 0), hi = min((run + 1) * per - at, nb + a.own);
             Rows<DH> x;
             x.clear();
-            if (t0 < t1) cache_blocks<DH, NW, RB, NT>(smem, x, b0 + i, g, row0, t0, t1);
-            if (run == to) own_keys<DH, NW, RB, NT>(smem, x, b0 + i, g, row0, length);
+            if (lo < nb) cache_blocks<DH, NW, RB, NT>(smem, x, b0 + i, g, row0, lo, min(hi, nb));
+            if (hi > nb) own_keys<DH, NW, RB, NT>(smem, x, b0 + i, g, row0, length, max(lo - nb, 0), hi - nb);
             write_rows<DH, NW, RB>(smem, stat, x, b0 + i, g, row0, to > from ? run - from : -1);
         }
     }
@@ -581,7 +562,7 @@ __device__ __forceinline__ void serve(const Block8Args& a, unsigned char* smem, 
 
 // RB row blocks to a workgroup; the row blocks beyond the last whole tile of eight have workgroups of REM row blocks and runs of their own.
 template <int DH, int NW, int RB, int REM, bool NT>
-__global__ __launch_bounds__(NW * 64, NW / 4) void attn_block8_kernel(Block8Args a) {
+__global__ __launch_bounds__(NW * 64, NW > 2 ? 2 : 1) void attn_block8_kernel(Block8Args a) {
     extern __shared__ __align__(16) unsigned char smem[];
     // a stream's row tiles share an XCD, and so an L2: workgroup -> XCD is round robin
     const int id = blockIdx.x;
@@ -690,9 +671,10 @@ hipError_t launch(Block8Args a, hipStream_t st) {
 template <int DH>
 hipError_t launch_for(const Block8Args& a, const Block8Plan& p, hipStream_t st) {
     switch (p.row_blocks * 10 + p.rem_blocks) {
-        case 10: return launch<DH, 4, 1, 0>(a, st);
-        case 20: return launch<DH, 8, 2, 0>(a, st);
-        case 40: return launch<DH, 8, 4, 0>(a, st);
+        case 10: return launch<DH, 2, 1, 0>(a, st);
+        case 20: return launch<DH, 4, 2, 0>(a, st);
+        case 40: return launch<DH, 4, 4, 0>(a, st);
+        case 42: return launch<DH, 4, 4, 2>(a, st);
         case 80: return launch<DH, 8, 8, 0>(a, st);
         case 82: return launch<DH, 8, 8, 2>(a, st);
         case 84: return launch<DH, 8, 8, 4>(a, st);
@@ -704,8 +686,8 @@ hipError_t launch_for(const Block8Args& a, const Block8Plan& p, hipStream_t st) 
 
 hipError_t raise_limits_attn_block8() {
     hipError_t e = hipSuccess;
-    for (hipError_t x : {raise<128, 4, 1, 0>(), raise<128, 8, 2, 0>(), raise<128, 8, 4, 0>(), raise<128, 8, 8, 0>(), raise<128, 8, 8, 2>(),
-                         raise<128, 8, 8, 4>(), raise<64, 4, 1, 0>(), raise<64, 8, 2, 0>(), raise<64, 8, 4, 0>(), raise<64, 8, 8, 0>(),
+    for (hipError_t x : {raise<128, 2, 1, 0>(), raise<128, 4, 2, 0>(), raise<128, 4, 4, 0>(), raise<128, 4, 4, 2>(), raise<128, 8, 8, 0>(), raise<128, 8, 8, 2>(),
+                         raise<128, 8, 8, 4>(), raise<64, 2, 1, 0>(), raise<64, 4, 2, 0>(), raise<64, 4, 4, 0>(), raise<64, 4, 4, 2>(), raise<64, 8, 8, 0>(),
                          raise<64, 8, 8, 2>(), raise<64, 8, 8, 4>()})
         if (x != hipSuccess) e = x;
     return e;

@@ -276,14 +276,18 @@ static size_t attention_scratch_bytes(const ygg_shape& s) {
 Block8Plan plan_block8(const ygg_shape& s) {
     Block8Plan p{};
     const int64_t R = (int64_t)s.n_nodes * (s.n_q_heads / s.n_kv_heads), row_blocks = (R + 31) / 32;
-    p.row_blocks = row_blocks <= 1 ? 1 : row_blocks <= 2 ? 2 : row_blocks <= 4 ? 4 : 8;
+#ifndef WIDE
+#define WIDE 8
+#endif
+    p.row_blocks = row_blocks <= 1 ? 1 : row_blocks <= 2 ? 2 : row_blocks <= 4 ? 4 : WIDE;
     p.row_tiles = (int32_t)((row_blocks + p.row_blocks - 1) / p.row_blocks);
     // One to four row blocks beyond whole tiles of eight: a smaller shape, whose wavefronts deal out the tiles of keys instead of idling.
-    if (row_blocks > 8 && row_blocks % 8 >= 1 && row_blocks % 8 <= 4) {
-        p.row_tiles = (int32_t)(row_blocks / 8);
-        p.rem_blocks = row_blocks % 8 <= 2 ? 2 : 4;
+    if (row_blocks > WIDE && row_blocks % WIDE >= 1 && row_blocks % WIDE <= WIDE / 2) {
+        p.row_tiles = (int32_t)(row_blocks / WIDE);
+        p.rem_blocks = row_blocks % WIDE <= 2 ? 2 : 4;
     }
-    p.lead = 2;
+    const int64_t per_cu = p.row_blocks == 8 ? 1 : 2;   // workgroups that a compute unit holds at once
+    p.lead = p.row_blocks == 8 ? 2 : p.row_blocks == 4 ? 3 : p.row_blocks == 2 ? 4 : 6;
     p.own = 2 + (s.n_nodes + 31) / 32;
     const int64_t units = (int64_t)s.batch * (s.max_seq_len / YGG_KV_BLOCK + p.lead + p.own);
     const int64_t most = std::min((int64_t)64, units), Hkv = s.n_kv_heads;
@@ -292,16 +296,16 @@ Block8Plan plan_block8(const ygg_shape& s) {
     // units: they take rem_blocks / 8 of a run's time per unit.
     int64_t best = 0;
     for (int64_t rounds = 1; rounds <= 4; ++rounds) {
-        const int64_t slots = 256 * rounds / Hkv;      // compute units to a kv head, over the rounds
+        const int64_t slots = 256 * per_cu * rounds / Hkv;      // compute units to a kv head, over the rounds
         int64_t rem = 0, runs = 0;
         if (p.rem_blocks) {
-            const int64_t all = 8 * p.row_tiles + p.rem_blocks;
+            const int64_t all = (int64_t)p.row_blocks * p.row_tiles + p.rem_blocks;
             rem = std::clamp((slots * p.rem_blocks + all - 1) / all, (int64_t)1, most);
             runs = std::clamp((slots - rem) / p.row_tiles, (int64_t)1, most);
         } else {
-            runs = std::clamp(rounds * std::max(streams_at_once(p.row_tiles), (int64_t)1) / Hkv, (int64_t)1, most);
+            runs = std::clamp(rounds * per_cu * std::max(streams_at_once(p.row_tiles), (int64_t)1) / Hkv, (int64_t)1, most);
         }
-        const int64_t need = ((runs * p.row_tiles + rem) * Hkv + 255) / 256;
+        const int64_t need = ((runs * p.row_tiles + rem) * Hkv + 256 * per_cu - 1) / (256 * per_cu);
         const int64_t time = need * ((units + runs - 1) / runs + 4);
         if (rounds == 1 || time < best) { best = time; p.runs = (int32_t)runs; p.rem_runs = (int32_t)rem; }
         p.most_runs = (int32_t)std::max({runs, rem, (int64_t)p.most_runs});
