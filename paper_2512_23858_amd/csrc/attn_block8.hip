@@ -30,6 +30,7 @@ namespace {
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
 
 constexpr int kT = YGG_KV_BLOCK;
 constexpr int kHeadroom = 7;    // weights of a block reach 2^7 (times v_scale's significand, below 2): E4M3 ends at 448
@@ -371,15 +372,14 @@ __device__ __forceinline__ void cache_blocks(unsigned char* smem, Rows<DH>& x, i
 #pragma unroll
     for (int j = 0; j < J; ++j) {
         u32x4 raw[4];
-        float top = 0.f;
+        u16x2 most = {};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             raw[k] = *reinterpret_cast<const u32x4*>(qp + 64 * j + 8 * k);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                top = fmaxf(top, fmaxf(fabsf(__uint_as_float(raw[k][e] << 16)), fabsf(__uint_as_float(raw[k][e] & 0xffff0000u))));
+            for (int e = 0; e < 4; ++e) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, raw[k][e] & 0x7fff7fffu));   // (bits are in the magnitudes' order)
         }
-        top = other_half_max(top);
+        const float top = other_half_max(__uint_as_float((uint32_t)max(most[0], most[1]) << 16));
         // the largest magnitude lands in [128, 256)
         const int up = min(kHeadroom + 127 - (int)(__float_as_uint(top) >> 23), 126);
         const float by = __uint_as_float((uint32_t)(up + 127) << 23);
@@ -391,7 +391,7 @@ __device__ __forceinline__ void cache_blocks(unsigned char* smem, Rows<DH>& x, i
                 const uint32_t u = raw[k][2 * e], v = raw[k][2 * e + 1];
                 const float y[4] = {__uint_as_float(u << 16) * by, __uint_as_float(u & 0xffff0000u) * by, __uint_as_float(v << 16) * by,
                                     __uint_as_float(v & 0xffff0000u) * by};
-                int hi = 0, lo = 0;
+                int hi = (int)u, lo = (int)v;    // (overwritten)
                 split4(y, hi, lo);
                 qhi[j][2 * k + e] = hi;
                 qlo[j][2 * k + e] = lo;
@@ -506,6 +506,11 @@ __device__ __forceinline__ void cache_blocks(unsigned char* smem, Rows<DH>& x, i
     int step = 0;
     for (; step < steps; step += 2) {
         advance(step, s0, s1, w1, w0);
+        if (step + 1 == steps) {   // an odd last step
+            w1 = w0;
+            ++step;
+            break;
+        }
         advance(step + 1, s1, s0, w0, w1);
     }
     dma_wait_keep<0>();
