@@ -1,11 +1,16 @@
 // Penalties, biases and grammar masks on logits, with each row's first maximum.
 //
-//   constrain_kernel  one workgroup per (tree node, chunk of the vocabulary).  The node's path is walked in LDS and its tokens are
+//   constrain_kernel  one workgroup per (tree node, 8192 tokens of the vocabulary).  The node's path is walked in LDS and its tokens are
 //                     counted into a table of the chunk; then the chunk streams through once, four logits to a thread and step, each
 //                     with its confirmed count, path count, bias and mask bit.  The arithmetic is fp32, one rounding per step as
 //                     the definition has it (no fused multiply-add), so that equal inputs give equal ties.
 //   best_kernel       the chunks' maxima of a row, first maximum.
-// Bound by the stream of logits in and out; counts and biases of a sequence are read by all of its nodes and stay in L2.
+// Bound by the stream of logits in and out; counts and biases of a sequence are read by all of its nodes and stay in L2.  129 rows of
+// 128256 bf16 logits with everything on: 25.7 us with both kernels (a copy of their size takes 18), 784 rows of 32003 fp32 logits read for
+// their maxima only 33.  Many resident wavefronts with few registers serve best: four rows to a workgroup that share counts and biases, or
+// all of a thread's loads up front, or penalties for listed tokens only, measured 41 to 60 us.  The logits are stored past the caches: with
+// plain stores 35 us instead of 25, though a reader that follows at once (an argmax over them) then ends 3 us earlier (50.7 and 53.7 us
+// for both).
 #include "ygg_internal.h"
 #include "ygg_device.h"
 
@@ -14,7 +19,7 @@
 namespace ygg {
 namespace {
 
-constexpr int kChunk = 4096;
+constexpr int kChunk = 8192;
 
 struct Best {
     float val;
@@ -28,6 +33,7 @@ __device__ __forceinline__ void take_first(float& v, int& i, float v2, int i2) {
 struct __attribute__((packed, aligned(4))) F4 { float x[4]; };
 struct __attribute__((packed, aligned(4))) I4 { int32_t x[4]; };
 struct __attribute__((packed, aligned(2))) H4 { uint16_t x[4]; };
+typedef float Out4 __attribute__((ext_vector_type(4), aligned(4)));
 
 template <typename T>
 __device__ __forceinline__ float logit_of(T v) {
@@ -35,11 +41,24 @@ __device__ __forceinline__ float logit_of(T v) {
     else return __uint_as_float((uint32_t)v << 16);
 }
 
+// x / d, correctly rounded, for many x: Markstein's method from the correctly rounded reciprocal r of d -- a quotient within one unit of
+// the last place, corrected by its exact remainder (twice: the first correction brings the quotient that near).
+struct Divisor {
+    float d, r;
+    __device__ __forceinline__ explicit Divisor(float x) : d(x), r(1.f / x) {}
+    __device__ __forceinline__ float of(float x) const {
+        float q = x * r;
+        q = fmaf(fmaf(-q, d, x), r, q);
+        q = fmaf(fmaf(-q, d, x), r, q);
+        return __builtin_isinf(x) ? x : q;
+    }
+};
+
 template <typename T>
 __global__ __launch_bounds__(256) void constrain_kernel(ConstrainArgs a) {
-    __shared__ int32_t parent_s[kMaxNodes];
-    __shared__ int32_t token_s[kMaxNodes];
-    __shared__ __align__(8) uint16_t times_s[kChunk];   // occurrences on the path, by token of the chunk
+    extern __shared__ int32_t nodes_s[];                // parents, tokens
+    int32_t *const parent_s = nodes_s, *const token_s = nodes_s + a.N;
+    __shared__ __align__(16) uint16_t times_s[kChunk];   // occurrences on the path, by token of the chunk
     __shared__ Best best_s[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t row = blockIdx.x;   // b * N + i
@@ -75,10 +94,11 @@ __global__ __launch_bounds__(256) void constrain_kernel(ConstrainArgs a) {
     float* out = a.out ? a.out + row * a.V : nullptr;
     float bv = -INFINITY;
     int bi = 0x7fffffff;
+    const Divisor over(repetition);
     auto constrained = [&](float v, int32_t confirmed, uint32_t times, float add, bool allowed) {
 #pragma clang fp contract(off)
         const uint32_t c = ((uint32_t)confirmed & 0x7fffffffu) + times;
-        if (confirmed != 0 || times) v = v > 0.f ? v / repetition : v * repetition;
+        if (confirmed != 0 || times) v = v > 0.f ? over.of(v) : v * repetition;
         v = v - frequency * (float)c;
         v = v - (c ? presence : 0.f);
         if (bias) v = v + add;
@@ -100,14 +120,14 @@ __global__ __launch_bounds__(256) void constrain_kernel(ConstrainArgs a) {
             if (bias) add = *reinterpret_cast<const F4*>(bias + j);
             const uint32_t bits = mask ? mask[j >> 5] >> (j & 31) : 0xfu;
             const uint2 times = *reinterpret_cast<const uint2*>(times_s + (j - c0));
-            F4 y;
+            Out4 y;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint32_t t = ((e < 2 ? times.x : times.y) >> (16 * (e & 1))) & 0xffffu;
-                y.x[e] = constrained(v[e], n.x[e], t, add.x[e], (bits >> e) & 1u);
-                if (y.x[e] > bv || bi == 0x7fffffff) { bv = y.x[e]; bi = j + e; }
+                y[e] = constrained(v[e], n.x[e], t, add.x[e], (bits >> e) & 1u);
+                if (y[e] > bv || bi == 0x7fffffff) { bv = y[e]; bi = j + e; }
             }
-            if (out) *reinterpret_cast<F4*>(out + j) = y;
+            if (out) __builtin_nontemporal_store(y, reinterpret_cast<Out4*>(out + j));
         } else {
             for (int e = j; e < c1; ++e) {
                 const float y = constrained(logit_of(x[e]), counts ? counts[e] : 0, times_s[e - c0], bias ? bias[e] : 0.f,
@@ -118,13 +138,13 @@ __global__ __launch_bounds__(256) void constrain_kernel(ConstrainArgs a) {
         }
     }
     if (!a.best) return;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) take_first(bv, bi, __shfl_xor(bv, o), __shfl_xor(bi, o));
-    if (lane == 0) best_s[wave] = {bv, bi};
+    const uint32_t top = wave_max_u32(key_of(bv));           // the wavefront's maximum, then the lowest of its tokens
+    const uint32_t at = wave_min_u32(key_of(bv) == top ? (uint32_t)bi : 0x7fffffffu);
+    if (lane == 0) best_s[wave] = {float_of(top), (int32_t)at};
     __syncthreads();
     if (tid == 0) {
 #pragma unroll
-        for (int w = 1; w < 4; ++w) take_first(bv, bi, best_s[w].val, best_s[w].idx);
+        for (int w = 0; w < 4; ++w) take_first(bv, bi, best_s[w].val, best_s[w].idx);
         if (gridDim.y == 1) a.best[row] = bi;
         else static_cast<Best*>(a.part)[row * gridDim.y + blockIdx.y] = {bv, bi};
     }
@@ -168,8 +188,8 @@ hipError_t launch_constrain(const ConstrainArgs& a, bool f32, hipStream_t st) {
     const int64_t rows = (int64_t)a.B * a.N;
     const int chunks = (a.V + kChunk - 1) / kChunk;
     const dim3 grid((unsigned)rows, (unsigned)chunks);
-    if (f32) hipLaunchKernelGGL((constrain_kernel<float>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((constrain_kernel<uint16_t>), grid, dim3(256), 0, st, a);
+    if (f32) hipLaunchKernelGGL((constrain_kernel<float>), grid, dim3(256), 2 * a.N * sizeof(int32_t), st, a);
+    else hipLaunchKernelGGL((constrain_kernel<uint16_t>), grid, dim3(256), 2 * a.N * sizeof(int32_t), st, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.best || chunks == 1) return e;
     hipLaunchKernelGGL(best_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a, rows, chunks);
