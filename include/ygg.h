@@ -323,7 +323,7 @@ int32_t ygg_tree_attention_block8(const ygg_shape *shape, const void *q, const y
  *   seq_lens     [B] int32: the lengths AFTER the append (only read; clamped to kv_capacity); tokens seq_lens[b] - n_new[b] ..
  *                seq_lens[b] - 1 are written
  * Rows of the open block go to the tail as they are; a block that is completed is encoded: scale = max|x| / 448 over its 64
- * tokens of one head (1 if all are zero, never below 2^-100), code = the E4M3 value nearest to x / scale, ties to even.
+ * tokens of one head (1 if all are zero, never below 2^-100), code = the E4M3 value nearest to x * (1 / scale) in fp32, ties to even.
  * Requires max_new <= n_rows unless rows is given.  Needs no workspace.
  */
 int32_t ygg_block8_append(const ygg_shape *shape, int32_t n_layers, const void *k_new, const void *v_new, int32_t n_rows,
