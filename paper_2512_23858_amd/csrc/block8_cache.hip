@@ -89,7 +89,11 @@ __global__ __launch_bounds__(256) void block8_append_kernel(AppendArgs a) {
             const int64_t r = new_row(token);
             return r >= 0 ? fresh_rows + r * row : nullptr;
         };
-        auto fetch = [](const uint16_t* p, int d) { return p ? *reinterpret_cast<const u32x4*>(p + d) : u32x4{}; };
+        auto fetch = [](const uint16_t* p, int d) {
+            u32x4 x = {};
+            if (p) x = *reinterpret_cast<const u32x4*>(p + d);
+            return x;
+        };
         u32x4 k[PT][2], v[4];
 #pragma unroll
         for (int u = 0; u < PT; ++u) {
@@ -152,9 +156,13 @@ __global__ __launch_bounds__(256) void block8_append_kernel(AppendArgs a) {
     for (int64_t p = tid; p < (end - open) * (DH / 8); p += 256) {
         const int64_t token = open + p / (DH / 8), r = new_row(token);
         const int64_t d = p % (DH / 8) * 8;
-        const uint4 zero = make_uint4(0, 0, 0, 0);
-        *reinterpret_cast<uint4*>(k_tail + token % (2 * kT) * row + d) = r >= 0 ? *reinterpret_cast<const uint4*>(k_new + r * row + d) : zero;
-        *reinterpret_cast<uint4*>(v_tail + token % (2 * kT) * row + d) = r >= 0 ? *reinterpret_cast<const uint4*>(v_new + r * row + d) : zero;
+        u32x4 k = {}, v = {};
+        if (r >= 0) {
+            k = *reinterpret_cast<const u32x4*>(k_new + r * row + d);
+            v = *reinterpret_cast<const u32x4*>(v_new + r * row + d);
+        }
+        *reinterpret_cast<u32x4*>(k_tail + token % (2 * kT) * row + d) = k;
+        *reinterpret_cast<u32x4*>(v_tail + token % (2 * kT) * row + d) = v;
     }
 }
 
