@@ -526,25 +526,29 @@ __device__ __forceinline__ void cache_blocks(unsigned char* smem, Rows<DH>& x, i
 }
 
 // The batch laid end to end, in units of a block's time: of each sequence a.lead empty units (what a segment costs beside its keys), its
-// full blocks, and a.own units for the tiles of its own keys.  Run r of `runs` has the units r * per .. (r + 1) * per - 1.
+// full blocks, and a.own units for the tiles of its own keys.  Run r of `runs` has the units r * per .. (r + 1) * per - 1; with runs == 0
+// each sequence is a workgroup's, and run says which.
 template <int DH, int NW, int RB, bool NT>
 __device__ __forceinline__ void serve(const Block8Args& a, unsigned char* smem, int g, int run, int runs, int row0, int32_t* seq_splits) {
     float* const stat = reinterpret_cast<float*>(smem + a.stat_at);
     const int lane = threadIdx.x & 63;
+    // runs == 0: a workgroup to each sequence, as the only run of a batch of one
+    const int begin = runs == 0 ? run : 0, end = runs == 0 ? run + 1 : a.B;
+    if (runs == 0) { run = 0; runs = 1; }
     auto length = [&](int b) {
-        const int L = b < a.B ? a.seq_lens[b] : 0;
+        const int L = b < end ? a.seq_lens[b] : 0;
         return L < 0 ? 0 : (L > a.max_seq_len ? a.max_seq_len : L);
     };
-    int L = length(lane);
-    int total = wave_sum_i32(L / kT);
-    for (int b0 = 64; b0 < a.B; b0 += 64) total += wave_sum_i32(length(b0 + lane) / kT);
-    total += a.B * (a.lead + a.own);
+    int L = length(begin + lane);
+    int total = end - begin == 1 ? __builtin_amdgcn_readfirstlane(L) / kT : wave_sum_i32(L / kT);
+    for (int b0 = begin + 64; b0 < end; b0 += 64) total += wave_sum_i32(length(b0 + lane) / kT);
+    total += (end - begin) * (a.lead + a.own);
     const int per = (total + runs - 1) / runs;
     int before = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-        if (b0 > 0) L = length(b0 + lane);
-        const int blocks = L / kT, units = b0 + lane < a.B ? a.lead + blocks + a.own : 0;
-        const int sums = wave_prefix_i32(units, lane);
+    for (int b0 = begin; b0 < end; b0 += 64) {
+        if (b0 > begin) L = length(b0 + lane);
+        const int blocks = L / kT, units = b0 + lane < end ? a.lead + blocks + a.own : 0;
+        const int sums = end - begin == 1 ? units : wave_prefix_i32(units, lane);
         const int first = before + sums - units + a.lead;            // unit of the first block
         before += __builtin_amdgcn_readlane(sums, 63);
         const int first_run = first / per, last_run = (first + blocks + a.own - 1) / per;
@@ -574,7 +578,7 @@ __global__ __launch_bounds__(NW * 64, NW > 2 ? 2 : 1) void attn_block8_kernel(Bl
     if (REM == 0 || id < a.main_groups) {
         const int xcd = id % 8, rest = id / 8;
         const int tile = rest % a.row_tiles, stream = rest / a.row_tiles * 8 + xcd;
-        if (stream >= a.runs * a.Hkv) return;
+        if (stream >= (a.runs ? a.runs : a.B) * a.Hkv) return;
         const int run = stream / a.Hkv, g = stream % a.Hkv;
         serve<DH, NW, RB, NT>(a, smem, g, run, a.runs, tile * RB * 32, stream == 0 && tile == 0 ? a.seq_splits : nullptr);
     } else if constexpr (REM > 0) {
@@ -658,13 +662,13 @@ hipError_t launch(Block8Args a, hipStream_t st) {
     if constexpr (REM > 0) smem = std::max(smem, Layout<DH, NW, REM>::smem(a.N));
     if (smem > kAttnMfmaMaxSmem) return hipErrorInvalidValue;
     a.stat_at = (int32_t)(smem - NW * 32 * 2 * sizeof(float));
-    const int64_t streams = (int64_t)a.runs * a.Hkv;
+    const int64_t streams = (int64_t)(a.runs ? a.runs : a.B) * a.Hkv;
     a.main_groups = (int32_t)((streams + 7) / 8 * 8 * a.row_tiles);
-    const dim3 grid((unsigned)(a.main_groups + (REM > 0 ? a.rem_runs * a.Hkv : 0)));
+    const dim3 grid((unsigned)(a.main_groups + (REM > 0 ? (a.rem_runs ? a.rem_runs : a.B) * a.Hkv : 0)));
     // the streaming hint where a workgroup is its stream's only reader
     if (a.row_tiles == 1 && REM == 0) hipLaunchKernelGGL((attn_block8_kernel<DH, NW, RB, REM, true>), grid, dim3(NW * 64), smem, st, a);
     else hipLaunchKernelGGL((attn_block8_kernel<DH, NW, RB, REM, false>), grid, dim3(NW * 64), smem, st, a);
-    if (const hipError_t e = hipGetLastError(); e != hipSuccess || (a.runs == 1 && (REM == 0 || a.rem_runs == 1))) return e;
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess || (a.runs <= 1 && a.rem_runs <= 1)) return e;   // (no sequence is cut)
     constexpr int LPR = DH / 8;
     auto groups = [&](int lanes) { return dim3((unsigned)(((int64_t)a.N * a.Hq * lanes + 255) / 256), (unsigned)a.B); };
     // few rows: a whole wavefront to each

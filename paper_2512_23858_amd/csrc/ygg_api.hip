@@ -289,32 +289,45 @@ Block8Plan plan_block8(const ygg_shape& s) {
     const int64_t per_cu = p.row_blocks == 8 ? 1 : 2;   // workgroups that a compute unit holds at once
     p.lead = p.row_blocks == 8 ? 2 : p.row_blocks == 4 ? 3 : p.row_blocks == 2 ? 4 : 6;
     p.own = 2 + (s.n_nodes + 31) / 32;
-    const int64_t units = (int64_t)s.batch * (s.max_seq_len / YGG_KV_BLOCK + p.lead + p.own);
+    const int64_t longest = s.max_seq_len / YGG_KV_BLOCK + p.own;      // units of a sequence
+    const int64_t units = (int64_t)s.batch * (longest + p.lead);
     const int64_t most = std::min((int64_t)64, units), Hkv = s.n_kv_heads;
-    // Runs: as many as fill the chip with whole rounds of workgroups (one to a compute unit), and of one to four rounds those that take
-    // least time, a round being the units of a run and a start.  Workgroups beyond the whole tiles share the first round's compute
-    // units: they take rem_blocks / 8 of a run's time per unit.
+    // Runs: as many as fill the chip with whole rounds of workgroups, and of one to four rounds those that take least time, a round being
+    // the units of a run and a start.  Workgroups beyond the whole tiles share the first round's compute units: they take rem_blocks / 8
+    // of a run's time per unit.
+    const int64_t slots = 256 * per_cu;
     int64_t best = 0;
     for (int64_t rounds = 1; rounds <= 4; ++rounds) {
-        const int64_t slots = 256 * per_cu * rounds / Hkv;      // compute units to a kv head, over the rounds
+        const int64_t at_once = slots * rounds / Hkv;      // workgroups to a kv head, over the rounds
         int64_t rem = 0, runs = 0;
         if (p.rem_blocks) {
             const int64_t all = (int64_t)p.row_blocks * p.row_tiles + p.rem_blocks;
-            rem = std::clamp((slots * p.rem_blocks + all - 1) / all, (int64_t)1, most);
-            runs = std::clamp((slots - rem) / p.row_tiles, (int64_t)1, most);
+            rem = std::clamp((at_once * p.rem_blocks + all - 1) / all, (int64_t)1, most);
+            runs = std::clamp((at_once - rem) / p.row_tiles, (int64_t)1, most);
         } else {
             runs = std::clamp(rounds * per_cu * std::max(streams_at_once(p.row_tiles), (int64_t)1) / Hkv, (int64_t)1, most);
         }
-        const int64_t need = ((runs * p.row_tiles + rem) * Hkv + 256 * per_cu - 1) / (256 * per_cu);
+        const int64_t need = ((runs * p.row_tiles + rem) * Hkv + slots - 1) / slots;
         const int64_t time = need * ((units + runs - 1) / runs + 4);
         if (rounds == 1 || time < best) { best = time; p.runs = (int32_t)runs; p.rem_runs = (int32_t)rem; }
         p.most_runs = (int32_t)std::max({runs, rem, (int64_t)p.most_runs});
     }
-    const int32_t nsplit = std::max(p.runs, p.rem_runs);
+    // A workgroup to each sequence where that ends sooner than runs and their merge (4.5 us).  Units take 0.5, 0.6, 1.0 and 1.8 us for one,
+    // two, four and eight row blocks where a workgroup has its compute unit to itself, and a little over half of that at head_dim 64.
+    const float unit = (p.row_blocks == 1 ? 0.5f : p.row_blocks == 2 ? 0.6f : p.row_blocks == 4 ? 1.0f : 1.8f) * (s.head_dim == 64 ? 0.6f : 1.f);
+    const int64_t groups = (int64_t)s.batch * Hkv * (p.row_tiles + (p.rem_blocks ? 1 : 0));
+    const int64_t rounds = (groups + slots - 1) / slots;
+    if (unit * (float)(rounds * (longest + 4)) < unit * (float)best + 4.5f) { p.runs = p.rem_runs = 0; }
+    const int32_t nsplit = std::max({p.runs, p.rem_runs, 1});
     p.part_o_bytes = part_o_bytes(s, true, nsplit);
     p.part_rec_bytes = part_rec_bytes(s, nsplit);
     p.seq_splits_bytes = align256(2 * (size_t)s.batch * sizeof(int32_t));
     return p;
+}
+
+// Workspace for this shape and every smaller max_seq_len: the most runs that any of them takes.
+static size_t block8_scratch_bytes(const ygg_shape& s, const Block8Plan& p) {
+    return part_o_bytes(s, true, p.most_runs) + part_rec_bytes(s, p.most_runs) + p.seq_splits_bytes;
 }
 
 // Raises the shared-memory limits of the current device's kernels once; later calls cost one atomic load.
@@ -396,8 +409,7 @@ size_t ygg_workspace_bytes(const ygg_shape* s, int32_t op, int32_t n_layers) {
         }
         case YGG_OP_ATTENTION_BLOCK8: {
             if (check_block8(s) != YGG_OK) return 0;
-            const Block8Plan p = plan_block8(*s);   // the most runs that this or a shorter bound may take
-            return part_o_bytes(*s, true, p.most_runs) + part_rec_bytes(*s, p.most_runs) + p.seq_splits_bytes;
+            return block8_scratch_bytes(*s, plan_block8(*s));
         }
         case YGG_OP_CONSTRAIN: {
             if (check_shape(s, false, true) != YGG_OK) return 0;
@@ -625,7 +637,7 @@ int32_t ygg_tree_attention_block8(const ygg_shape* s, const void* q, const ygg_b
     // the kernels count query rows, workgroups and a batch's blocks with 31 bits
     if (rows > 0x7fffffffLL || ((int64_t)p.runs + p.rem_runs + 8) * s->n_kv_heads * p.row_tiles > 0x7fffffffLL ||
         (int64_t)s->batch * (s->max_seq_len / YGG_KV_BLOCK + p.lead + p.own) > 0x3fffffffLL) return YGG_ERR_UNSUPPORTED;
-    if (int32_t rc = check_workspace(workspace, workspace_bytes, p.part_o_bytes + p.part_rec_bytes + p.seq_splits_bytes)) return rc;
+    if (int32_t rc = check_workspace(workspace, workspace_bytes, block8_scratch_bytes(*s, p))) return rc;
     if (int32_t rc = ensure_device_ready()) return rc;
 
     Block8Args a{};
