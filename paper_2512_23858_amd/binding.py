@@ -207,12 +207,13 @@ def _kv_torch_dtype(shape: Shape):
     return {F32: torch.float32, BF16: torch.bfloat16, FP8_E4M3: torch.uint8, FP8_BLOCK: torch.bfloat16}[shape.kv_dtype]
 
 
-def _explain(shape: Shape, *checks):
+def _explain(shape: Shape, *checks, sizes=()):
     """The native module refused an argument: run the same checks here, which raise what the caller should see.
-    checks: (tensor or None, wanted dtype or None, name)."""
+    checks: (tensor or None, wanted dtype or None, name); sizes: as for _explain_sizes."""
     shape.c()
     for t, dtype, name in checks:
         _dev(t, dtype, name)
+    _explain_sizes(*sizes)
     raise TypeError("an argument is neither a tensor nor None, or a number is out of range")
 
 
@@ -328,7 +329,7 @@ def accept_and_compact(shape: Shape, n_layers: int, parent_idx, token_ids, k_tre
         _check(rc, "ygg_accept_and_compact")
 
 
-def _explain_rows(shape, rows, *checks):
+def _explain_rows(shape, rows, *checks, sizes=()):
     """_explain for calls with tensors whose rows may be strided: rows = (tensor, wanted dtype or None, name)."""
     for t, dtype, name in rows:
         if t is None:
@@ -344,7 +345,25 @@ def _explain_rows(shape, rows, *checks):
     for t, _, name in rows:
         if t is not None and not t.is_contiguous():
             raise ValueError(f"{name}: rows must be dense and lie evenly over batch and tokens")
-    _explain(shape)
+    _explain(shape, sizes=sizes)
+
+
+def _explain_sizes(*sizes):
+    """sizes: (tensor or None, elements that the shape asks for, name); of strided rows, the exact shape instead of a number."""
+    for t, n, name in sizes:
+        if t is None:
+            continue
+        if isinstance(n, tuple):
+            if tuple(t.shape[:2]) != n[:2] or t.numel() != n[0] * n[1] * n[2]:
+                raise ValueError(f"{name}: {n[0]} x {n[1]} rows of {n[2]} elements are wanted, got {tuple(t.shape)}")
+        elif t.numel() < n:
+            raise ValueError(f"{name}: {n} elements are wanted, got {t.numel()}")
+
+
+def _cache_sizes(shape: Shape, cache: BlockCache, layers: int):
+    heads, nblk = layers * shape.batch * shape.n_kv_heads, -(-shape.kv_capacity // KV_BLOCK)
+    want = [heads * nblk * KV_BLOCK * shape.head_dim] * 2 + [heads * nblk] * 2 + [heads * 2 * KV_BLOCK * shape.head_dim] * 2
+    return list(zip(cache.tensors(), want, ("k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail")))
 
 
 def _cache_checks(cache: BlockCache):
@@ -359,9 +378,13 @@ def tree_attention_block8(shape: Shape, q, cache: BlockCache, seq_lens, k_tree, 
     if rc:
         if rc < 0:
             bf, i32 = torch.bfloat16, torch.int32
+            nodes, q_row, kv_row = shape.batch * shape.n_nodes, shape.n_q_heads * shape.head_dim, shape.n_kv_heads * shape.head_dim
             _explain(shape, (q, bf, "q"), *_cache_checks(cache), (seq_lens, i32, "seq_lens"), (k_tree, bf, "k_tree"),
                      (v_tree, bf, "v_tree"), (parent_idx, i32, "parent_idx"), (out, bf, "out"), (lse, torch.float32, "lse"),
-                     (workspace, None, "workspace"))
+                     (workspace, None, "workspace"),
+                     sizes=[(q, nodes * q_row, "q"), *_cache_sizes(shape, cache, 1), (seq_lens, shape.batch, "seq_lens"),
+                            (k_tree, nodes * kv_row, "k_tree"), (v_tree, nodes * kv_row, "v_tree"), (parent_idx, nodes, "parent_idx"),
+                            (out, nodes * q_row, "out"), (lse, nodes * shape.n_q_heads, "lse")])
         _check(rc, "ygg_tree_attention_block8")
     return out
 
@@ -374,8 +397,11 @@ def block8_append(shape: Shape, n_layers: int, k_new, v_new, cache: BlockCache, 
     if rc:
         if rc < 0:
             bf, i32 = torch.bfloat16, torch.int32
+            new = n_layers * shape.batch * (k_new.shape[2] if k_new is not None and k_new.dim() > 2 else 0) * shape.n_kv_heads * shape.head_dim
             _explain(shape, (k_new, bf, "k_new"), (v_new, bf, "v_new"), (rows, i32, "rows"), (n_new, i32, "n_new"),
-                     (seq_lens, i32, "seq_lens"), *_cache_checks(cache))
+                     (seq_lens, i32, "seq_lens"), *_cache_checks(cache),
+                     sizes=[(k_new, new, "k_new"), (v_new, new, "v_new"), (n_new, shape.batch, "n_new"), (seq_lens, shape.batch, "seq_lens"),
+                            (rows, 0 if rows is None else shape.batch * rows.shape[-1], "rows"), *_cache_sizes(shape, cache, n_layers)])
         _check(rc, "ygg_block8_append")
 
 
@@ -388,9 +414,14 @@ def tree_rotary(shape: Shape, q, k, q_out, k_out, frequencies, seq_lens=None, pa
     if rc:
         if rc < 0:
             dt, i32 = torch.float32 if shape.kv_dtype == F32 else torch.bfloat16, torch.int32
+            B, N = shape.batch, shape.n_nodes
             _explain_rows(shape, ((q, dt, "q"), (k, dt, "k")), (q_out, dt, "q_out"), (k_out, dt, "k_out"),
                           (frequencies, torch.float64, "frequencies"), (seq_lens, i32, "seq_lens"), (parent_idx, i32, "parent_idx"),
-                          (positions, i32, "positions"))
+                          (positions, i32, "positions"),
+                          sizes=[(q, (B, N, shape.n_q_heads * shape.head_dim), "q"), (k, (B, N, shape.n_kv_heads * shape.head_dim), "k"),
+                                 (q_out, B * N * shape.n_q_heads * shape.head_dim, "q_out"),
+                                 (k_out, B * N * shape.n_kv_heads * shape.head_dim, "k_out"), (seq_lens, B, "seq_lens"),
+                                 (parent_idx, B * N, "parent_idx"), (positions, B * N, "positions")])
         _check(rc, "ygg_tree_rotary")
 
 
@@ -400,7 +431,9 @@ def count_tokens(shape: Shape, tokens, n_new, counts, rows=None, first: int = 0,
     if rc:
         if rc < 0:
             i32 = torch.int32
-            _explain(shape, (tokens, i32, "tokens"), (n_new, i32, "n_new"), (counts, i32, "counts"), (rows, i32, "rows"))
+            _explain(shape, (tokens, i32, "tokens"), (n_new, i32, "n_new"), (counts, i32, "counts"), (rows, i32, "rows"),
+                     sizes=[(tokens, shape.batch * tokens.shape[-1], "tokens"), (n_new, shape.batch, "n_new"),
+                            (counts, shape.batch * shape.vocab, "counts"), (rows, 0 if rows is None else shape.batch * rows.shape[-1], "rows")])
         _check(rc, "ygg_count_tokens")
 
 
@@ -413,12 +446,18 @@ def constrain_logits(shape: Shape, logits, parent_idx, token_ids, out=None, best
     if rc:
         if rc < 0:
             f32, i32 = torch.float32, torch.int32
+            B, V, nodes = shape.batch, shape.vocab, shape.batch * shape.n_nodes
             if logits is not None and logits.dtype not in (f32, torch.bfloat16):
                 raise TypeError(f"logits: expected {f32} or {torch.bfloat16}, got {logits.dtype}")
             _explain_rows(shape, ((logits, None, "logits"),), (parent_idx, i32, "parent_idx"), (token_ids, i32, "token_ids"),
                           (out, f32, "out"), (best, i32, "best"), (counts, i32, "counts"), (repetition, f32, "repetition"),
                           (presence, f32, "presence"), (frequency, f32, "frequency"), (bias, f32, "bias"), (masks, i32, "masks"),
-                          (mask_index, i32, "mask_index"), (workspace, None, "workspace"))
+                          (mask_index, i32, "mask_index"), (workspace, None, "workspace"),
+                          sizes=[(logits, (B, shape.n_nodes, V), "logits"), (parent_idx, nodes, "parent_idx"), (token_ids, nodes, "token_ids"),
+                                 (out, nodes * V, "out"), (best, nodes, "best"), (counts, B * V, "counts"), (repetition, B, "repetition"),
+                                 (presence, B, "presence"), (frequency, B, "frequency"),
+                                 (bias, V if bias is not None and bias.dim() == 1 else B * V, "bias"),
+                                 (masks, 0 if masks is None else masks.shape[0] * (-(-V // 32)), "masks"), (mask_index, nodes, "mask_index")])
         _check(rc, "ygg_constrain_logits")
 
 

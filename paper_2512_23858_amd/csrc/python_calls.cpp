@@ -101,6 +101,16 @@ struct Args {
         if (B > 1 && N > 1 && t.stride(0) != N * stride) { ok = false; return nullptr; }
         return t.data_ptr();
     }
+    // A given tensor has at least so many elements (the kernels go by the shape, not by the tensors)
+    void holds(int i, int64_t n) {
+        if (ok && a[i] != Py_None && THPVariable_Unpack(a[i]).numel() < n) ok = false;
+    }
+    // .. and these leading dimensions, with `inner` elements behind them
+    void rows_are(int i, int64_t B, int64_t N, int64_t inner) {
+        if (!ok || a[i] == Py_None) return;
+        const at::Tensor& t = THPVariable_Unpack(a[i]);
+        ok = t.size(0) == B && t.size(1) == N && t.numel() == B * N * inner;
+    }
     int32_t size(int i, int64_t d) {   // of a tensor that passed its check, else 0
         if (!ok || a[i] == Py_None) return 0;
         const at::Tensor& t = THPVariable_Unpack(a[i]);
@@ -253,12 +263,18 @@ PyObject* accept_and_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// The six tensors of a block cache, from argument i on
-ygg_block8_cache block_cache(Args& t, int i) {
+// The six tensors of a block cache of so many layers, from argument i on
+ygg_block8_cache block_cache(Args& t, int i, const ygg_shape& s, int64_t layers) {
     ygg_block8_cache c{};
     c.k_codes = t.ptr(i, at::kByte); c.v_codes = t.ptr(i + 1, at::kByte);
     c.k_scale = t.floats(i + 2); c.v_scale = t.floats(i + 3);
     c.k_tail = t.ptr(i + 4, at::kBFloat16); c.v_tail = t.ptr(i + 5, at::kBFloat16);
+    const int64_t heads = layers * s.batch * s.n_kv_heads, nblk = (s.kv_capacity + YGG_KV_BLOCK - 1) / YGG_KV_BLOCK;
+    for (int k = 0; k < 2; ++k) {
+        t.holds(i + k, heads * nblk * YGG_KV_BLOCK * s.head_dim);
+        t.holds(i + 2 + k, heads * nblk);
+        t.holds(i + 4 + k, heads * 2 * YGG_KV_BLOCK * s.head_dim);
+    }
     return c;
 }
 
@@ -268,12 +284,16 @@ PyObject* tree_attention_block8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     ygg_shape s{};
     Args t{a};
     t.ok = read_shape(a[0], s);
-    const ygg_block8_cache c = block_cache(t, 2);
+    const ygg_block8_cache c = block_cache(t, 2, s, 1);
     void *q = t.ptr(1, at::kBFloat16), *kt = t.ptr(9, at::kBFloat16), *vt = t.ptr(10, at::kBFloat16), *out = t.ptr(12, at::kBFloat16);
     int32_t *lens = t.ints(8), *parent = t.ints(11);
     float* lse = t.floats(13);
     size_t wn;
     void* ws = t.scratch(14, wn);
+    const int64_t nodes = (int64_t)s.batch * s.n_nodes;
+    for (int i : {1, 12}) t.holds(i, nodes * s.n_q_heads * s.head_dim);
+    for (int i : {9, 10}) t.holds(i, nodes * s.n_kv_heads * s.head_dim);
+    t.holds(8, s.batch); t.holds(11, nodes); t.holds(13, nodes * s.n_q_heads);
     return finish(t.ok, [&](void* st) { return ygg_tree_attention_block8(&s, q, &c, lens, kt, vt, parent, out, lse, ws, wn, st); });
 }
 
@@ -287,8 +307,10 @@ PyObject* block8_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     t.number(1, layers);
     void *k = t.ptr(2, at::kBFloat16), *v = t.ptr(3, at::kBFloat16);
     int32_t *rows = t.ints(4), *n_new = t.ints(5), *lens = t.ints(6);
-    const ygg_block8_cache c = block_cache(t, 7);
+    const ygg_block8_cache c = block_cache(t, 7, s, layers);
     const int32_t n_rows = t.size(2, 2), most = rows ? t.size(4, 1) : n_rows;
+    for (int i : {2, 3}) t.holds(i, (int64_t)layers * s.batch * n_rows * s.n_kv_heads * s.head_dim);
+    t.holds(4, (int64_t)s.batch * most); t.holds(5, s.batch); t.holds(6, s.batch);
     return finish(t.ok, [&](void* st) { return ygg_block8_append(&s, layers, k, v, n_rows, rows, most, n_new, lens, &c, st); });
 }
 
@@ -304,6 +326,9 @@ PyObject* tree_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const double* f = t.typed<double>(5, at::kDouble);
     const int32_t pairs = t.size(5, 0);
     int32_t *lens = t.ints(6), *parent = t.ints(7), *positions = t.ints(8);
+    const int64_t B = s.batch, N = s.n_nodes, q_row = (int64_t)s.n_q_heads * s.head_dim, k_row = (int64_t)s.n_kv_heads * s.head_dim;
+    t.rows_are(1, B, N, q_row); t.rows_are(2, B, N, k_row);
+    t.holds(3, B * N * q_row); t.holds(4, B * N * k_row); t.holds(6, B); t.holds(7, B * N); t.holds(8, B * N);
     const bool interleaved = a[9] == Py_True;
     const double scale = PyFloat_AsDouble(a[10]);
     if (PyErr_Occurred()) { PyErr_Clear(); t.ok = false; }
@@ -322,6 +347,7 @@ PyObject* count_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int32_t first = 0;
     t.number(5, first);
     const int32_t n_tokens = t.size(1, 1), most = rows ? t.size(4, 1) : n_tokens;
+    t.holds(1, (int64_t)s.batch * n_tokens); t.holds(2, s.batch); t.holds(3, (int64_t)s.batch * s.vocab); t.holds(4, (int64_t)s.batch * most);
     const bool prompt = a[6] == Py_True;
     return finish(t.ok, [&](void* st) { return ygg_count_tokens(&s, tokens, n_tokens, rows, first, most, n_new, prompt, counts, st); });
 }
@@ -349,6 +375,11 @@ PyObject* constrain_logits(PyObject*, PyObject* const* a, Py_ssize_t n) {
     r.masks = reinterpret_cast<const uint32_t*>(t.ints(11));
     r.n_masks = t.size(11, 0);
     r.mask_index = t.ints(12);
+    const int64_t B = s.batch, nodes = B * s.n_nodes, V = s.vocab;
+    t.rows_are(1, B, s.n_nodes, V);
+    for (int i : {2, 3, 5, 12}) t.holds(i, nodes);
+    for (int i : {7, 8, 9}) t.holds(i, B);
+    t.holds(4, nodes * V); t.holds(6, B * V); t.holds(10, r.bias_shared ? V : B * V); t.holds(11, r.n_masks * ((V + 31) / 32));
     size_t wn;
     void* ws = t.scratch(13, wn);
     return finish(t.ok, [&](void* st) { return ygg_constrain_logits(&s, x, dt, stride, parent, token, &r, out, best, ws, wn, st); });

@@ -316,3 +316,27 @@ def test_refusals_on_the_gpu_binding():
         ygg.tree_attention_block8(plain_shape, *args, workspace=ws)
     with pytest.raises(RuntimeError, match="unsupported"):      # and the other calls do not take the block type
         ygg.tree_attention(s, args[0], args[3], args[4], args[2], args[3], args[4], args[5], args[6], workspace=ws)
+
+
+def test_tensors_smaller_than_the_shape_are_refused():
+    p = _problem(2, 4, 2, 64, 3, [70, 10], seed=1)
+    s, c, i32 = p["shape"], p["cache"], dict(dtype=torch.int32, device=DEV)
+    ws = workspace(s, ygg.OP_ATTENTION_BLOCK8)
+    lens = torch.tensor([70, 10], **i32)
+    good = dict(q=p["q"], cache=c, seq_lens=lens, k_tree=p["dense"]["k_tree"], v_tree=p["dense"]["v_tree"], parent_idx=to_dev(p["parent"]),
+                out=torch.empty_like(p["q"]), lse=torch.empty((2, 3, 4), device=DEV), workspace=ws)
+    ygg.tree_attention_block8(s, **good)
+    for name in ("q", "seq_lens", "k_tree", "v_tree", "parent_idx", "out", "lse"):
+        with pytest.raises(ValueError, match=name):
+            ygg.tree_attention_block8(s, **{**good, name: good[name][:1]})
+    for name in ("k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail"):
+        bad = ygg.BlockCache(*c.tensors())
+        setattr(bad, name, getattr(c, name)[:1])
+        with pytest.raises(ValueError, match=name):
+            ygg.tree_attention_block8(s, **{**good, "cache": bad})
+    k = torch.zeros((1, 2, 5, 2, 64), dtype=torch.bfloat16, device=DEV)
+    n = torch.tensor([1, 1], **i32)
+    one = ygg.BlockCache(*(t[None] for t in c.tensors()))
+    for kw in (dict(v_new=k[:, :1]), dict(n_new=n[:1]), dict(seq_lens=n[:1]), dict(rows=torch.zeros((1, 3), **i32)), dict(n_layers=2)):
+        with pytest.raises(ValueError, match=next(iter(kw)) if "n_layers" not in kw else "k_new"):
+            ygg.block8_append(s, **{**dict(n_layers=1, k_new=k, v_new=k, cache=one, seq_lens=n, n_new=n), **kw})

@@ -99,3 +99,6 @@ def test_refusals_on_the_gpu_binding():
     wide = torch.zeros((1, 4, 3, 64), dtype=torch.bfloat16, device=DEV)
     with pytest.raises(RuntimeError, match="inconsistent"):      # in place needs dense tokens
         ygg.tree_rotary(shape, wide[:, :, :2], None, wide, None, f, positions=pos)
+    for kw in (dict(q=q[:, :3]), dict(q_out=q[:, :3].contiguous()), dict(positions=pos[:, :2].contiguous())):
+        with pytest.raises(ValueError, match=next(iter(kw))):
+            ygg.tree_rotary(shape, **{**dict(q=q, k=None, q_out=q.clone(), k_out=None, frequencies=f, positions=pos), **kw})
