@@ -72,7 +72,8 @@ typedef enum {
     YGG_FP8_E4M3 = 2,  /* K and V (cache and tree) as 8-bit E4M3 codes, Q and O bf16; head_dim 128;
                           accepted by ygg_tree_attention_fp8kv and ygg_accept_and_compact only */
     YGG_FP8_BLOCK = 3  /* the cache is a ygg_block8_cache, everything else is bf16; accepted by
-                          ygg_tree_attention_block8, ygg_block8_append and ygg_tree_rotary */
+                          ygg_tree_attention_block8, ygg_block8_append and ygg_tree_rotary, and by
+                          ygg_accept_and_compact with n_layers = 0 */
 } ygg_dtype;
 
 typedef enum {
@@ -307,7 +308,8 @@ typedef struct {
  * A tree of one node (n_nodes 1, depth 0) is plain decoding.  The keys and values of cache and tree must be finite.
  *   q, out [B,N,Hq,Dh] bf16;  k_tree, v_tree [B,N,Hkv,Dh] bf16;  lse [B,N,Hq] fp32 or NULL;  seq_lens, parent_idx int32
  * q (bf16, 8 bits of significand) and the softmax weights enter the products as sums of two E4M3 values, that is with 8 bits and
- * an exponent per row and tile; scores, softmax and accumulation are fp32.  Workspace: ygg_workspace_bytes(ATTENTION_BLOCK8).
+ * an exponent per row and tile; softmax and accumulation are fp32 (the matrix instructions of 8-bit values cut each product at
+ * 2^-13 of the largest of its group before they add).  Workspace: ygg_workspace_bytes(ATTENTION_BLOCK8).
  */
 int32_t ygg_tree_attention_block8(const ygg_shape *shape, const void *q, const ygg_block8_cache *cache /* host struct */,
                                   const int32_t *seq_lens, const void *k_tree, const void *v_tree,
@@ -317,7 +319,7 @@ int32_t ygg_tree_attention_block8(const ygg_shape *shape, const void *q, const y
 /*
  * Appends new tokens to such a cache, all layers in one launch: the K/V bookkeeping that ygg_accept_and_compact does for plain
  * caches (call it with n_layers = 0 and hand its accept_path, accept_len and seq_lens to this), or a prompt's K/V.
- *   k_new, v_new [n_layers,B,n_rows,Hkv,Dh] bf16: the tree's, or the prompt's, rows
+ *   k_new, v_new [n_layers,B,n_rows,Hkv,Dh] bf16: the tree's, or the prompt's, rows, finite
  *   rows         [B,max_new] int32: token k of the new ones is row rows[b][k]; NULL: row k.  Out-of-range rows count as zeros
  *   n_new        [B] int32: new tokens of sequence b, 0 .. max_new (clamped to that)
  *   seq_lens     [B] int32: the lengths AFTER the append (only read; clamped to kv_capacity); tokens seq_lens[b] - n_new[b] ..
@@ -364,7 +366,7 @@ int32_t ygg_count_tokens(const ygg_shape *shape, const int32_t *tokens, int32_t 
  *     if v occurs in counts[b] (reply or prompt) or on the path:  x <- x > 0 ? x / repetition[b] : x * repetition[b]
  *     x <- x - frequency[b] * c;   if c > 0:  x <- x - presence[b];   x <- x + bias[b][v]
  *     if mask_index[b][i] = m >= 0 and bit v%32 of masks[m][v/32] is 0:  x <- -inf
- *     out[b,i,v] = x;   best[b,i] = argmax_v x (first maximum)
+ *     out[b,i,v] = x;   best[b,i] = argmax_v x (first maximum; a NaN that no mask covers counts as the largest value)
  * `out` feeds ygg_equal_growth_expand / _attach and ygg_accept_and_compact, `best` the latter's target_tokens.
  */
 typedef struct {

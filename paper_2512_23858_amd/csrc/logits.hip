@@ -15,18 +15,23 @@
 #include "ygg_device.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ygg {
 namespace {
 
 constexpr int kChunk = 8192;
 
+// A row's (or a chunk's) maximum: larger values have larger keys, the two zeros the same one, a NaN the largest.
 struct Best {
-    float val;
+    uint32_t key;
     int32_t idx;
 };
-__device__ __forceinline__ void take_first(float& v, int& i, float v2, int i2) {
-    if (v2 > v || (v2 == v && i2 < i)) { v = v2; i = i2; }
+__device__ __forceinline__ uint32_t rank_of(float v) { return v != v ? 0xffffffffu : key_of(v + 0.f); }   // (-0 + 0 = 0)
+// The largest key in the wavefront, and the lowest index that has it.
+__device__ __forceinline__ Best first_of_wave(uint32_t key, int32_t idx) {
+    const uint32_t top = wave_max_u32(key);
+    return {top, (int32_t)wave_min_u32(key == top ? (uint32_t)idx : 0x7fffffffu)};
 }
 
 // Rows start at any element, so vectors are only as aligned as their elements.
@@ -41,17 +46,20 @@ __device__ __forceinline__ float logit_of(T v) {
     else return __uint_as_float((uint32_t)v << 16);
 }
 
-// x / d, correctly rounded, for many x: Markstein's method from the correctly rounded reciprocal r of d -- a quotient within one unit of
-// the last place, corrected by its exact remainder (twice: the first correction brings the quotient that near).
+// x / d, correctly rounded, for many x > 0: Markstein's method from the correctly rounded reciprocal r of d -- a quotient within one unit
+// of the last place, corrected by its exact remainder (twice: the first correction brings the quotient that near).  It holds for d from
+// 2^-32 to 2^32 and quotients from 2^-64 to 2^120, where no remainder (a multiple of 2^(-64-23-32-23) = 2^-142) leaves fp32's range; others
+// want the division itself.
 struct Divisor {
     float d, r;
-    __device__ __forceinline__ explicit Divisor(float x) : d(x), r(1.f / x) {}
+    uint32_t span;      // of the bits of such quotients; 0: no quotient by this d
+    __device__ __forceinline__ explicit Divisor(float x) : d(x), r(1.f / x), span(x >= 0x1p-32f && x <= 0x1p32f ? (uint32_t)(120 + 64) << 23 : 0) {}
     __device__ __forceinline__ float of(float x) const {
         float q = x * r;
         q = fmaf(fmaf(-q, d, x), r, q);
-        q = fmaf(fmaf(-q, d, x), r, q);
-        return __builtin_isinf(x) ? x : q;
+        return fmaf(fmaf(-q, d, x), r, q);
     }
+    __device__ __forceinline__ bool fails(float q) const { return __float_as_uint(q) - ((127u - 64) << 23) >= span; }
 };
 
 template <typename T>
@@ -93,17 +101,29 @@ __global__ __launch_bounds__(256) void constrain_kernel(ConstrainArgs a) {
     const float* bias = a.bias ? a.bias + (a.bias_shared ? 0 : (int64_t)b * a.V) : nullptr;
     float* out = a.out ? a.out + row * a.V : nullptr;
     float bv = -INFINITY;
-    int bi = 0x7fffffff;
+    int bi = c0 + 4 * tid < c1 ? c0 + 4 * tid : 0x7fffffff;
+    auto consider = [&](float y, int j) {   // the first maximum, or the first NaN
+        if (!(y <= bv) && bv == bv) { bv = y; bi = j; }
+    };
     const Divisor over(repetition);
-    auto constrained = [&](float v, int32_t confirmed, uint32_t times, float add, bool allowed) {
+    bool again = false;    // a quotient was none: these logits once more, with divisions
+    auto constrained = [&](auto divide, float v, int32_t confirmed, uint32_t times, float add, bool allowed) {
 #pragma clang fp contract(off)
         const uint32_t c = ((uint32_t)confirmed & 0x7fffffffu) + times;
-        if (confirmed != 0 || times) v = v > 0.f ? over.of(v) : v * repetition;
+        float q;
+        if constexpr (divide) q = v / repetition;
+        else {
+            q = over.of(v);
+            again |= v > 0.f && over.fails(q);
+        }
+        if (confirmed != 0 || times) v = v > 0.f ? q : v * repetition;
         v = v - frequency * (float)c;
         v = v - (c ? presence : 0.f);
         if (bias) v = v + add;
         return allowed ? v : -INFINITY;
     };
+    typedef std::integral_constant<bool, false> Quotients;
+    typedef std::integral_constant<bool, true> Divisions;
     for (int j = c0 + 4 * tid; j < c1; j += 1024) {
         if (j + 4 <= c1) {
             float v[4];
@@ -121,32 +141,39 @@ __global__ __launch_bounds__(256) void constrain_kernel(ConstrainArgs a) {
             const uint32_t bits = mask ? mask[j >> 5] >> (j & 31) : 0xfu;
             const uint2 times = *reinterpret_cast<const uint2*>(times_s + (j - c0));
             Out4 y;
+            auto all = [&](auto divide) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t t = ((e < 2 ? times.x : times.y) >> (16 * (e & 1))) & 0xffffu;
-                y[e] = constrained(v[e], n.x[e], t, add.x[e], (bits >> e) & 1u);
-                if (y[e] > bv || bi == 0x7fffffff) { bv = y[e]; bi = j + e; }
-            }
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t t = ((e < 2 ? times.x : times.y) >> (16 * (e & 1))) & 0xffffu;
+                    y[e] = constrained(divide, v[e], n.x[e], t, add.x[e], (bits >> e) & 1u);
+                }
+            };
+            again = false;
+            all(Quotients{});
+            if (again) all(Divisions{});
+#pragma unroll
+            for (int e = 0; e < 4; ++e) consider(y[e], j + e);
             if (out) __builtin_nontemporal_store(y, reinterpret_cast<Out4*>(out + j));
         } else {
             for (int e = j; e < c1; ++e) {
-                const float y = constrained(logit_of(x[e]), counts ? counts[e] : 0, times_s[e - c0], bias ? bias[e] : 0.f,
+                const float y = constrained(Divisions{}, logit_of(x[e]), counts ? counts[e] : 0, times_s[e - c0], bias ? bias[e] : 0.f,
                                             !mask || ((mask[e >> 5] >> (e & 31)) & 1u));
-                if (y > bv || bi == 0x7fffffff) { bv = y; bi = e; }
+                consider(y, e);
                 if (out) out[e] = y;
             }
         }
     }
     if (!a.best) return;
-    const uint32_t top = wave_max_u32(key_of(bv));           // the wavefront's maximum, then the lowest of its tokens
-    const uint32_t at = wave_min_u32(key_of(bv) == top ? (uint32_t)bi : 0x7fffffffu);
-    if (lane == 0) best_s[wave] = {float_of(top), (int32_t)at};
+    const Best mine = first_of_wave(rank_of(bv), bi);
+    if (lane == 0) best_s[wave] = mine;
     __syncthreads();
     if (tid == 0) {
+        Best best = mine;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) take_first(bv, bi, best_s[w].val, best_s[w].idx);
-        if (gridDim.y == 1) a.best[row] = bi;
-        else static_cast<Best*>(a.part)[row * gridDim.y + blockIdx.y] = {bv, bi};
+        for (int w = 1; w < 4; ++w)
+            if (best_s[w].key > best.key || (best_s[w].key == best.key && best_s[w].idx < best.idx)) best = best_s[w];
+        if (gridDim.y == 1) a.best[row] = best.idx;
+        else static_cast<Best*>(a.part)[row * gridDim.y + blockIdx.y] = best;
     }
 }
 
@@ -155,19 +182,18 @@ __global__ __launch_bounds__(256) void best_kernel(ConstrainArgs a, int64_t rows
     const int lane = threadIdx.x & 63;
     if (row >= rows) return;
     const Best* p = static_cast<const Best*>(a.part) + row * chunks;
-    float bv = -INFINITY;
-    int bi = 0x7fffffff;
-    for (int c = lane; c < chunks; c += 64) take_first(bv, bi, p[c].val, p[c].idx);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) take_first(bv, bi, __shfl_xor(bv, o), __shfl_xor(bi, o));
-    if (lane == 0) a.best[row] = bi;
+    Best best = {0, 0x7fffffff};
+    for (int c = lane; c < chunks; c += 64)
+        if (p[c].key > best.key) best = p[c];   // (a lane's chunks come in order)
+    best = first_of_wave(best.key, best.idx);
+    if (lane == 0) a.best[row] = best.idx;
 }
 
 __global__ __launch_bounds__(256) void count_kernel(CountArgs a) {
     const int b = blockIdx.y;
     const int n = min(a.n_new[b], a.max_new);
-    for (int k = blockIdx.x * 256 + threadIdx.x; k < n; k += gridDim.x * 256) {
-        const int64_t r = a.rows ? (int64_t)a.rows[(int64_t)b * a.max_new + k] : (int64_t)a.first + k;
+    for (int64_t k = blockIdx.x * 256 + threadIdx.x; k < n; k += gridDim.x * 256) {
+        const int64_t r = a.rows ? (int64_t)a.rows[(int64_t)b * a.max_new + k] : a.first + k;
         if (r < 0 || r >= a.n_tokens) continue;
         const int t = a.tokens[(int64_t)b * a.n_tokens + r];
         if (t < 0 || t >= a.V) continue;
@@ -197,7 +223,7 @@ hipError_t launch_constrain(const ConstrainArgs& a, bool f32, hipStream_t st) {
 }
 
 hipError_t launch_count(const CountArgs& a, hipStream_t st) {
-    const unsigned groups = (unsigned)std::clamp((a.max_new + 255) / 256, 1, 64);
+    const unsigned groups = (unsigned)std::clamp(((int64_t)a.max_new + 255) / 256, (int64_t)1, (int64_t)64);
     hipLaunchKernelGGL(count_kernel, dim3(groups, (unsigned)a.B), dim3(256), 0, st, a);
     return hipGetLastError();
 }

@@ -177,3 +177,60 @@ def test_refusals_on_the_gpu_binding():
         ygg.constrain_logits(shape, wide[..., :100], i, i, out=wide[..., :100])
     with pytest.raises(TypeError, match="counts"):
         ygg.count_tokens(shape, i, torch.ones(1, dtype=torch.int32, device=DEV), x)
+
+
+def test_tensors_smaller_than_the_shape_are_refused():
+    shape = _shape(2, 3, 100)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    good = dict(logits=torch.zeros((2, 3, 100), device=DEV), parent_idx=torch.full((2, 3), -1, **i32), token_ids=torch.zeros((2, 3), **i32),
+                out=torch.zeros((2, 3, 100), device=DEV), best=torch.zeros((2, 3), **i32), counts=torch.zeros((2, 100), **i32),
+                repetition=torch.ones(2, device=DEV), presence=torch.ones(2, device=DEV), frequency=torch.ones(2, device=DEV),
+                bias=torch.zeros((2, 100), device=DEV), masks=torch.zeros((2, 4), **i32), mask_index=torch.zeros((2, 3), **i32),
+                workspace=workspace(shape, ygg.OP_CONSTRAIN))
+    ygg.constrain_logits(shape, **good)
+    for name in good:
+        if name not in ("workspace", "masks"):
+            with pytest.raises(ValueError, match=name):
+                ygg.constrain_logits(shape, **{**good, name: good[name][:1]})
+    with pytest.raises(ValueError, match="masks"):
+        ygg.constrain_logits(shape, **{**good, "masks": torch.zeros((2, 3), **i32)})
+    t, n = torch.zeros((2, 7), **i32), torch.ones(2, **i32)
+    for args, kw, name in (((t[:1], n, good["counts"]), {}, "tokens"), ((t, n[:1], good["counts"]), {}, "n_new"),
+                           ((t, n, good["counts"][:1]), {}, "counts"), ((t, n, good["counts"]), dict(rows=t[:1]), "rows")):
+        with pytest.raises(ValueError, match=name):
+            ygg.count_tokens(shape, *args, **kw)
+
+
+def test_zeros_of_both_signs_are_equal_and_a_nan_is_the_largest():
+    x = torch.full((1, 5, 9000), -1.0)
+    x[0, 0, 4000], x[0, 0, 4500], x[0, 0, 8800] = -0.0, 0.0, 0.0
+    x[0, 1, 3], x[0, 1, 100], x[0, 1, 8999] = 0.0, -0.0, 0.0
+    x[0, 2, 5], x[0, 2, 7000], x[0, 2, 7001], x[0, 2, 8500] = float("inf"), float("nan"), 9.0, -float("nan")
+    x[0, 3, 0], x[0, 3, 1], x[0, 3, 8999] = float("nan"), float("nan"), 3.0
+    x[0, 4, 600], x[0, 4, 8704], x[0, 4, 8705] = float("nan"), -float("nan"), 0.5
+    masks = np.full((1, 282), -1, np.int32)
+    masks[0, 600 // 32] &= ~(1 << (600 % 32))
+    masks[0, 8704 // 32] &= ~(1 << (8704 % 32))
+    h = dict(logits=x, parent=np.array([[-1, 0, 1, 2, 3]], np.int32), token=np.zeros((1, 5), np.int32), counts=None, repetition=None,
+             presence=None, frequency=None, bias=None, masks=masks, mask_index=np.array([[-1, -1, -1, -1, 0]], np.int32))
+    out, best = _run(h)
+    assert np.array_equal(out, _ref({**h, "repetition": np.ones(1, np.float32), "presence": np.zeros(1, np.float32),
+                                     "frequency": np.zeros(1, np.float32)}), equal_nan=True)
+    assert np.array_equal(best, [[4000, 3, 7000, 0, 8705]])
+
+
+def test_quotients_at_the_ends_of_the_range_are_the_rounded_ones():
+    """The division by the repetition penalty, bit for bit, where the quotient or the remainder leaves the range of normal numbers."""
+    V = 4003
+    g = np.random.default_rng(8)
+    repetition = np.array([1e-40, 1e-3, 0.5, 0.7, 1.3, 3.0, 1e30, 1.7e38, 3.4e38], np.float32)
+    B = len(repetition)
+    x = np.exp2(g.uniform(-149, 128, (B, 1, V))).astype(np.float32)
+    x[:, 0, :5] = [np.inf, 0.0, 1e-45, np.finfo(np.float32).max, np.finfo(np.float32).tiny]
+    h = dict(logits=torch.from_numpy(x), parent=np.full((B, 1), -1, np.int32), token=np.full((B, 1), -1, np.int32),
+             counts=np.full((B, V), -2 ** 31, np.int32), repetition=repetition, presence=np.zeros(B, np.float32),
+             frequency=np.zeros(B, np.float32), bias=None, masks=None, mask_index=np.full((B, 1), -1, np.int32))
+    with np.errstate(over="ignore"):
+        ref = _ref(h)
+    out, best = _run(h)
+    assert _same(out, ref) and np.array_equal(best, ref.argmax(-1))
