@@ -683,7 +683,6 @@ hipError_t launch_for(const Block8Args& a, const Block8Plan& p, hipStream_t st) 
         case 10: return launch<DH, 2, 1, 0>(a, st);
         case 20: return launch<DH, 4, 2, 0>(a, st);
         case 40: return launch<DH, 4, 4, 0>(a, st);
-        case 42: return launch<DH, 4, 4, 2>(a, st);
         case 80: return launch<DH, 8, 8, 0>(a, st);
         case 82: return launch<DH, 8, 8, 2>(a, st);
         case 84: return launch<DH, 8, 8, 4>(a, st);
@@ -695,8 +694,8 @@ hipError_t launch_for(const Block8Args& a, const Block8Plan& p, hipStream_t st) 
 
 hipError_t raise_limits_attn_block8() {
     hipError_t e = hipSuccess;
-    for (hipError_t x : {raise<128, 2, 1, 0>(), raise<128, 4, 2, 0>(), raise<128, 4, 4, 0>(), raise<128, 4, 4, 2>(), raise<128, 8, 8, 0>(), raise<128, 8, 8, 2>(),
-                         raise<128, 8, 8, 4>(), raise<64, 2, 1, 0>(), raise<64, 4, 2, 0>(), raise<64, 4, 4, 0>(), raise<64, 4, 4, 2>(), raise<64, 8, 8, 0>(),
+    for (hipError_t x : {raise<128, 2, 1, 0>(), raise<128, 4, 2, 0>(), raise<128, 4, 4, 0>(), raise<128, 8, 8, 0>(), raise<128, 8, 8, 2>(),
+                         raise<128, 8, 8, 4>(), raise<64, 2, 1, 0>(), raise<64, 4, 2, 0>(), raise<64, 4, 4, 0>(), raise<64, 8, 8, 0>(),
                          raise<64, 8, 8, 2>(), raise<64, 8, 8, 4>()})
         if (x != hipSuccess) e = x;
     return e;

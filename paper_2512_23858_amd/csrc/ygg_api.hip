@@ -276,15 +276,15 @@ static size_t attention_scratch_bytes(const ygg_shape& s) {
 Block8Plan plan_block8(const ygg_shape& s) {
     Block8Plan p{};
     const int64_t R = (int64_t)s.n_nodes * (s.n_q_heads / s.n_kv_heads), row_blocks = (R + 31) / 32;
-#ifndef WIDE
-#define WIDE 8
-#endif
-    p.row_blocks = row_blocks <= 1 ? 1 : row_blocks <= 2 ? 2 : row_blocks <= 4 ? 4 : WIDE;
+    // As many row blocks to a stream of keys as registers hold: for the 1284 rows of 321 nodes behind 32768 tokens eight take 165 us and
+    // four 171.
+    p.row_blocks = row_blocks <= 1 ? 1 : row_blocks <= 2 ? 2 : row_blocks <= 4 ? 4 : 8;
     p.row_tiles = (int32_t)((row_blocks + p.row_blocks - 1) / p.row_blocks);
-    // One to four row blocks beyond whole tiles of eight: a smaller shape, whose wavefronts deal out the tiles of keys instead of idling.
-    if (row_blocks > WIDE && row_blocks % WIDE >= 1 && row_blocks % WIDE <= WIDE / 2) {
-        p.row_tiles = (int32_t)(row_blocks / WIDE);
-        p.rem_blocks = row_blocks % WIDE <= 2 ? 2 : 4;
+    // One to four row blocks beyond whole tiles of eight: a smaller shape, whose wavefronts deal out the tiles of keys instead of idling
+    // (those 1284 rows are five tiles and one row block: 166 us, as six tiles 212).
+    if (row_blocks > 8 && row_blocks % 8 >= 1 && row_blocks % 8 <= 4) {
+        p.row_tiles = (int32_t)(row_blocks / 8);
+        p.rem_blocks = row_blocks % 8 <= 2 ? 2 : 4;
     }
     const int64_t per_cu = p.row_blocks == 8 ? 1 : 2;   // workgroups that a compute unit holds at once
     p.lead = p.row_blocks == 8 ? 2 : p.row_blocks == 4 ? 3 : p.row_blocks == 2 ? 4 : 6;
@@ -634,8 +634,9 @@ int32_t ygg_tree_attention_block8(const ygg_shape* s, const void* q, const ygg_b
     if (!aligned16(q) || !aligned16(k_tree) || !aligned16(v_tree) || !aligned16(out)) return YGG_ERR_UNSUPPORTED;
     const int64_t rows = (int64_t)s->batch * s->n_nodes * s->n_q_heads;
     const Block8Plan p = plan_block8(*s);
-    // the kernels count query rows, workgroups and a batch's blocks with 31 bits
-    if (rows > 0x7fffffffLL || ((int64_t)p.runs + p.rem_runs + 8) * s->n_kv_heads * p.row_tiles > 0x7fffffffLL ||
+    // the kernels count query rows and a batch's blocks with 31 bits, and a launch's threads with 32
+    const int64_t streams = (p.runs ? (int64_t)p.runs + p.rem_runs : (int64_t)s->batch) * s->n_kv_heads + 8;
+    if (rows > 0x7fffffffLL || streams * (p.row_tiles + 1) > (1 << 22) || (int64_t)s->n_nodes * s->n_q_heads > (1 << 25) ||
         (int64_t)s->batch * (s->max_seq_len / YGG_KV_BLOCK + p.lead + p.own) > 0x3fffffffLL) return YGG_ERR_UNSUPPORTED;
     if (int32_t rc = check_workspace(workspace, workspace_bytes, block8_scratch_bytes(*s, p))) return rc;
     if (int32_t rc = ensure_device_ready()) return rc;
@@ -672,7 +673,7 @@ int32_t ygg_block8_append(const ygg_shape* s, int32_t n_layers, const void* k_ne
     a.nblk = (s->kv_capacity + YGG_KV_BLOCK - 1) / YGG_KV_BLOCK; a.cap = s->kv_capacity;
     a.n_layers = n_layers; a.B = s->batch; a.Hkv = s->n_kv_heads; a.n_rows = n_rows; a.max_new = max_new;
     a.blocks = (int32_t)(((int64_t)max_new + YGG_KV_BLOCK - 1) / YGG_KV_BLOCK);
-    if ((int64_t)n_layers * a.B * a.Hkv > 0x7fffffffLL / a.blocks) return YGG_ERR_UNSUPPORTED;
+    if ((int64_t)n_layers * a.B * a.Hkv > (1 << 23) / a.blocks) return YGG_ERR_UNSUPPORTED;   // (the launch grid)
     return launch_block8_append(a, s->head_dim, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? YGG_OK : YGG_ERR_LAUNCH;
 }
 
@@ -701,7 +702,7 @@ int32_t ygg_tree_rotary(const ygg_shape* s, const void* q, int64_t q_stride, con
     a.q_stride = q_stride; a.k_stride = k_stride;
     a.B = s->batch; a.N = s->n_nodes; a.Hq = q ? s->n_q_heads : 0; a.Hkv = k ? s->n_kv_heads : 0; a.Dh = s->head_dim;
     const int64_t units = ((int64_t)a.Hq + a.Hkv) * (a.Dh / 16);
-    if (units > (1 << 22)) return YGG_ERR_UNSUPPORTED;
+    if (units > (1 << 22) || s->n_nodes > (1 << 25)) return YGG_ERR_UNSUPPORTED;   // (the launch grid)
     a.units = (int32_t)units;
     a.rotary_dim = rotary_dim; a.max_seq_len = s->max_seq_len; a.scale = scale;
     return launch_rotary(a, f32, interleaved != 0, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? YGG_OK : YGG_ERR_LAUNCH;
@@ -730,7 +731,7 @@ int32_t ygg_constrain_logits(const ygg_shape* s, const void* logits, int32_t log
     if (rules->masks && !rules->mask_index) return YGG_ERR_NULL;
     if (rules->masks && rules->n_masks < 1) return YGG_ERR_SHAPE;
     const int64_t rows = (int64_t)s->batch * s->n_nodes;
-    if (rows > 0x7fffffffLL || s->vocab > (1 << 28)) return YGG_ERR_UNSUPPORTED;   // (the launch grid)
+    if (rows > (1 << 23) || s->vocab > (1 << 28)) return YGG_ERR_UNSUPPORTED;   // (the launch grid)
     if (best)
         if (int32_t rc = check_workspace(workspace, workspace_bytes, constrain_scratch_bytes(*s))) return rc;
     ConstrainArgs a{};

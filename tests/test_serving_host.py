@@ -151,6 +151,15 @@ def test_scratch_of_the_longest_prefix_serves_the_shorter_ones():
                 assert sizes[0] > 0 and sizes == sorted(sizes)
 
 
+def test_launches_beyond_the_grid_are_refused():
+    big = dict(batch=65535, n_q_heads=512, n_kv_heads=512, max_seq_len=0, kv_capacity=4)     # a workgroup to each sequence and head
+    assert _call("ygg_tree_attention_block8", _shape(**big), [FAKE, _cache(), FAKE, FAKE, FAKE, FAKE, FAKE, None, FAKE, BIG]) == UNSUPPORTED
+    assert _call("ygg_block8_append", _shape(batch=65535), [64, FAKE, FAKE, 13, FAKE, 65, FAKE, FAKE, _cache()]) == UNSUPPORTED
+    assert _call("ygg_tree_rotary", _shape(n_nodes=(1 << 25) + 1), [FAKE, 0, FAKE, 0, FAKE, FAKE, FAKE, 128, 0, 1.0, None, None, FAKE]) == UNSUPPORTED
+    assert _call("ygg_constrain_logits", _shape(batch=65535, n_nodes=1000),
+                 [FAKE, ygg.F32, 0, FAKE, FAKE, _Rules(), FAKE, FAKE, FAKE, BIG]) == UNSUPPORTED
+
+
 def test_frequencies():
     f = ygg.rotary_frequencies(128)
     assert f.dtype == torch.float64 and f.shape == (64,) and f[0] == 1 and math.isclose(f[63], 10000 ** (-126 / 128))
