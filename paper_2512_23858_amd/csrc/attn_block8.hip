@@ -478,7 +478,7 @@ __device__ __forceinline__ void cache_blocks(unsigned char* smem, Rows<DH>& x, i
                 w.lo[U * GROUPS + k] = lo;
                 sum += (p[k][0] + p[k][1]) + (p[k][2] + p[k][3]);
             }
-            op = after;
+            if constexpr (U + 1 < UNITS) op = after;
             __builtin_amdgcn_sched_barrier(0);
         });
         x.l = fmaf(sum, ldexpf(__builtin_amdgcn_rcpf(significand), max(w.c - x.ref, -127)), x.l);
@@ -647,13 +647,19 @@ __global__ __launch_bounds__(256) void block8_merge_kernel(Block8Args a) {
     if (a.lse && col == 0) a.lse[r] = m * kLn2 + logf(l);
 }
 
+// Up to four row blocks there is one row tile, and beyond eight there are several.
+template <int RB>
+constexpr bool kOneReader = RB < 8;
+template <int REM>
+constexpr bool kManyReaders = REM > 0;
+
 template <int DH, int NW, int RB, int REM>
 hipError_t raise() {
-    hipError_t e = hipSuccess;
-    for (const void* f : {reinterpret_cast<const void*>(&attn_block8_kernel<DH, NW, RB, REM, false>),
-                          reinterpret_cast<const void*>(&attn_block8_kernel<DH, NW, RB, REM, true>)})
-        if (const hipError_t x = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kAttnMfmaMaxSmem); x != hipSuccess) e = x;
-    return e;
+    auto limit = [](auto kernel) { return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kAttnMfmaMaxSmem); };
+    hipError_t e = hipSuccess, f = hipSuccess;
+    if constexpr (!kManyReaders<REM>) e = limit(&attn_block8_kernel<DH, NW, RB, REM, true>);
+    if constexpr (!kOneReader<RB>) f = limit(&attn_block8_kernel<DH, NW, RB, REM, false>);
+    return e != hipSuccess ? e : f;
 }
 
 template <int DH, int NW, int RB, int REM>
@@ -666,8 +672,10 @@ hipError_t launch(Block8Args a, hipStream_t st) {
     a.main_groups = (int32_t)((streams + 7) / 8 * 8 * a.row_tiles);
     const dim3 grid((unsigned)(a.main_groups + (REM > 0 ? (a.rem_runs ? a.rem_runs : a.B) * a.Hkv : 0)));
     // the streaming hint where a workgroup is its stream's only reader
-    if (a.row_tiles == 1 && REM == 0) hipLaunchKernelGGL((attn_block8_kernel<DH, NW, RB, REM, true>), grid, dim3(NW * 64), smem, st, a);
-    else hipLaunchKernelGGL((attn_block8_kernel<DH, NW, RB, REM, false>), grid, dim3(NW * 64), smem, st, a);
+    if constexpr (!kManyReaders<REM>)
+        if (kOneReader<RB> || a.row_tiles == 1) hipLaunchKernelGGL((attn_block8_kernel<DH, NW, RB, REM, true>), grid, dim3(NW * 64), smem, st, a);
+    if constexpr (!kOneReader<RB>)
+        if (kManyReaders<REM> || a.row_tiles > 1) hipLaunchKernelGGL((attn_block8_kernel<DH, NW, RB, REM, false>), grid, dim3(NW * 64), smem, st, a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess || (a.runs <= 1 && a.rem_runs <= 1)) return e;   // (no sequence is cut)
     constexpr int LPR = DH / 8;
     auto groups = [&](int lanes) { return dim3((unsigned)(((int64_t)a.N * a.Hq * lanes + 255) / 256), (unsigned)a.B); };
@@ -680,9 +688,9 @@ hipError_t launch(Block8Args a, hipStream_t st) {
 template <int DH>
 hipError_t launch_for(const Block8Args& a, const Block8Plan& p, hipStream_t st) {
     switch (p.row_blocks * 10 + p.rem_blocks) {
-        case 10: return launch<DH, 2, 1, 0>(a, st);
-        case 20: return launch<DH, 4, 2, 0>(a, st);
-        case 40: return launch<DH, 4, 4, 0>(a, st);
+        case 10: return p.wide ? launch<DH, 4, 1, 0>(a, st) : launch<DH, 2, 1, 0>(a, st);
+        case 20: return p.wide ? launch<DH, 8, 2, 0>(a, st) : launch<DH, 4, 2, 0>(a, st);
+        case 40: return p.wide ? launch<DH, 8, 4, 0>(a, st) : launch<DH, 4, 4, 0>(a, st);
         case 80: return launch<DH, 8, 8, 0>(a, st);
         case 82: return launch<DH, 8, 8, 2>(a, st);
         case 84: return launch<DH, 8, 8, 4>(a, st);
@@ -690,15 +698,20 @@ hipError_t launch_for(const Block8Args& a, const Block8Plan& p, hipStream_t st) 
     }
 }
 
+template <int DH>
+hipError_t raise_for() {
+    hipError_t e = hipSuccess;
+    for (hipError_t x : {raise<DH, 2, 1, 0>(), raise<DH, 4, 2, 0>(), raise<DH, 4, 4, 0>(), raise<DH, 4, 1, 0>(), raise<DH, 8, 2, 0>(),
+                         raise<DH, 8, 4, 0>(), raise<DH, 8, 8, 0>(), raise<DH, 8, 8, 2>(), raise<DH, 8, 8, 4>()})
+        if (x != hipSuccess) e = x;
+    return e;
+}
+
 }  // namespace
 
 hipError_t raise_limits_attn_block8() {
-    hipError_t e = hipSuccess;
-    for (hipError_t x : {raise<128, 2, 1, 0>(), raise<128, 4, 2, 0>(), raise<128, 4, 4, 0>(), raise<128, 8, 8, 0>(), raise<128, 8, 8, 2>(),
-                         raise<128, 8, 8, 4>(), raise<64, 2, 1, 0>(), raise<64, 4, 2, 0>(), raise<64, 4, 4, 0>(), raise<64, 8, 8, 0>(),
-                         raise<64, 8, 8, 2>(), raise<64, 8, 8, 4>()})
-        if (x != hipSuccess) e = x;
-    return e;
+    const hipError_t e = raise_for<128>(), f = raise_for<64>();
+    return e != hipSuccess ? e : f;
 }
 
 hipError_t launch_attn_block8(const Block8Args& a, const Block8Plan& p, int head_dim, hipStream_t st) {

@@ -313,11 +313,21 @@ Block8Plan plan_block8(const ygg_shape& s) {
         p.most_runs = (int32_t)std::max({runs, rem, (int64_t)p.most_runs});
     }
     // A workgroup to each sequence where that ends sooner than runs and their merge (4.5 us).  Units take 0.5, 0.6, 1.0 and 1.8 us for one,
-    // two, four and eight row blocks where a workgroup has its compute unit to itself, and a little over half of that at head_dim 64.
+    // two, four and eight row blocks where a workgroup has its compute unit to itself, and a little over half of that at head_dim 64.  It is
+    // no later either where all sequences at their bound take memory longer than the longest takes its workgroup (8 x 4096 tokens on 32 kv
+    // heads 72 -> 68 us, from 2000 to 4096 tokens 58 -> 52, 400 to 4096 49 -> 48), up to 4096 tokens or so: of 700 to 8192 the longest ends
+    // at 89 us and runs at 74.
     const float unit = (p.row_blocks == 1 ? 0.5f : p.row_blocks == 2 ? 0.6f : p.row_blocks == 4 ? 1.0f : 1.8f) * (s.head_dim == 64 ? 0.6f : 1.f);
     const int64_t groups = (int64_t)s.batch * Hkv * (p.row_tiles + (p.rem_blocks ? 1 : 0));
     const int64_t rounds = (groups + slots - 1) / slots;
-    if (unit * (float)(rounds * (longest + 4)) < unit * (float)best + 4.5f) { p.runs = p.rem_runs = 0; }
+    const float whole = unit * (float)(rounds * (longest + 4));
+    const float stream = 2.f * (float)s.batch * (float)s.max_seq_len * (float)Hkv * (float)s.head_dim / 5.2e6f;   // us
+    if (whole < unit * (float)best + 4.5f || (groups <= 256 && longest <= 72 && whole < stream)) {
+        p.runs = p.rem_runs = 0;
+        // with a compute unit to itself a workgroup takes twice the wavefronts, unless there is little to deal out to them (one token and 367
+        // tokens for 16 requests 14.2 -> 11.9 us, five nodes behind 5 x 627 18.1 -> 14.9; 61 behind 3 x 139 would go 14.6 -> 16.6)
+        p.wide = groups <= 256 && p.row_blocks < 8 && s.max_seq_len / YGG_KV_BLOCK >= 4;
+    }
     const int32_t nsplit = std::max({p.runs, p.rem_runs, 1});
     p.part_o_bytes = part_o_bytes(s, true, nsplit);
     p.part_rec_bytes = part_rec_bytes(s, nsplit);

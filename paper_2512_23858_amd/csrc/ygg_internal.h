@@ -161,6 +161,7 @@ struct Block8Plan {
     int32_t row_blocks;   // 32-row blocks to a workgroup: 1, 2, 4 or 8
     int32_t row_tiles;    // workgroups of that shape along the N*G query rows of one kv head
     int32_t rem_blocks;   // 2 or 4: the rows beyond them go to workgroups of that many row blocks; 0: there are none
+    bool wide;            // (runs == 0 only) twice the wavefronts to a workgroup
     int32_t runs, rem_runs;   // equal runs of the batch's keys per (kv head, row tile), one workgroup each, at most 64; 0: one to a sequence
     int32_t most_runs;    // the most that this or a shorter bound on the lengths may take
     int32_t lead, own;    // what a segment costs beside its keys, in blocks, and the tiles of a sequence's own keys

@@ -229,6 +229,15 @@ def test_attention_shapes(B, Hq, Hkv, Dh, N, lens):
     _check(p, *_attend(p))
 
 
+@pytest.mark.parametrize("Dh", [64, 128])
+@pytest.mark.parametrize("G,N", [(4, 1), (1, 32), (4, 9), (1, 64), (4, 17), (2, 61)])
+@pytest.mark.parametrize("lens", [[256], [700, 0, 319], [5, 1, 255, 64]])
+def test_attention_with_a_compute_unit_to_each_sequence(Dh, G, N, lens):
+    """Bounds from four blocks on with few sequences: the keys of one are dealt out to many wavefronts, some of which get none."""
+    p = _problem(len(lens), 2 * G, 2, Dh, N, lens, seed=N + len(lens), cap=max(max(lens), 256))
+    _check(p, *_attend(p))
+
+
 def test_attention_widest_tree_and_longest_chain():
     for tree in ("random", "chain"):
         p = _problem(1, 2, 1, 128, 1024, [100], seed=6, tree=tree)
