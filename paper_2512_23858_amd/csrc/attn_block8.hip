@@ -422,7 +422,7 @@ __device__ __forceinline__ void cache_blocks(unsigned char* smem, Rows<DH>& x, i
     const float scale = a.scale * kLog2e;
     const float *const ksp = a.k_scale + stream, *const vsp = a.v_scale + stream;
     float ks_next = uniform_load(ksp + tile_of(0)), vs_next = uniform_load(vsp + tile_of(0));
-    auto advance = [&](int step, f32x16 (&s)[2], f32x16 (&next)[2], const Weights& old, Weights& w) {
+    auto advance = [&](int step, f32x16 (&s)[2], f32x16 (&next)[2], Weights& old, Weights& w) {
         dma_wait_keep<0>();
         meet();
         fill(step + 2, step);
@@ -439,7 +439,9 @@ __device__ __forceinline__ void cache_blocks(unsigned char* smem, Rows<DH>& x, i
         const bool there = step < mine;        // (uniform) beyond this share's last tile all weights are zero
         const float by = ks * scale;
         w.c = there ? (int)ceilf(top * by) - kHeadroom : x.ref;
-        if (step == 0) x.ref = w.c;
+        // The first tile's power is the reference, and also that of the weights before it: they are zeros, but their product's scale is a
+        // byte whose 255 is a NaN, and old.c - x.ref has to lie in its range, -127 (clamped) to kRescale.
+        if (step == 0) x.ref = old.c = w.c;
         x.refer_to(w.c);
         // v_scale = significand * 2^ve: the significand joins the weights, the power is V's block scale
         const uint32_t vb = __float_as_uint(vs);
@@ -498,7 +500,7 @@ __device__ __forceinline__ void cache_blocks(unsigned char* smem, Rows<DH>& x, i
     f32x16 s0[2], s1[2];
     Weights w0, w1;
     w0.hi = w0.lo = w1.hi = w1.lo = i32x8{};
-    w1.c = 0;
+    w1.c = 0;    // (as x.ref: the reference of rows that no wavefront advances)
     w1.ve = 127;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
