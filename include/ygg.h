@@ -289,8 +289,11 @@ int32_t ygg_accept_and_compact(const ygg_shape *shape, int32_t n_layers,
  *   k_tail,  v_tail  [B,128,Hkv,Dh] bf16: the row of token p is p % 128
  *
  * With L = seq_lens[b], tokens 0 .. 64*(L/64) - 1 are read from the blocks and the last L % 64 from the tail; nothing else of a
- * cache is read.  A block is written once, when its last token arrives, from the bf16 rows of all its tokens.  The tail holds two
- * blocks, so seq_lens[b] may be taken back to any token of the block before the open one that has not been overwritten since.
+ * cache is read.  A block is written when its last token arrives, from the bf16 rows of all its tokens.  The tail keeps rows while
+ * their block is open: those with which an append completes a block go into codes only.  So seq_lens[b] may be taken back to any
+ * token of the open block, to any multiple of 64, and in the block before the open one up to the length from which the append that
+ * completed it began, where that lies in the block and no rows of a later block have come into its half of the tail since.  No
+ * other length finds its rows.
  * Inside a block the codes lie in the order in which the matrix instructions of gfx950 take them, so that a block is streamed as
  * it is stored: with token t (0..63) and dimension d, the code is at byte 1024*chunk + 16*lane + e,
  *   K: chunk = 2*((t/32)*(Dh/64) + d/64) + d/16%2,  lane = 32*(d/32%2) + t%32,  e = d%16

@@ -391,7 +391,8 @@ def tree_attention_block8(shape: Shape, q, cache: BlockCache, seq_lens, k_tree, 
 
 def block8_append(shape: Shape, n_layers: int, k_new, v_new, cache: BlockCache, seq_lens, n_new, rows=None):
     """ygg_block8_append: tokens seq_lens - n_new .. seq_lens - 1 of every layer, from rows of k_new and v_new
-    [n_layers,B,n_rows,Hkv,Dh]; rows [B,max_new] picks them (an accept_path), else they are the first n_new."""
+    [n_layers,B,n_rows,Hkv,Dh]; rows [B,max_new] picks them (an accept_path), else they are the first n_new.
+    include/ygg.h (ygg_block8_cache) says to which lengths a sequence can be taken back."""
     rc = (_native or _calls()).block8_append(shape, n_layers, k_new, v_new, rows, n_new, seq_lens, cache.k_codes, cache.v_codes,
                                              cache.k_scale, cache.v_scale, cache.k_tail, cache.v_tail)
     if rc:

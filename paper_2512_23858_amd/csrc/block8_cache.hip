@@ -153,7 +153,8 @@ __global__ __launch_bounds__(256) void block8_append_kernel(AppendArgs a) {
         }
     }
     if (j > 0) return;
-    // rows that stay open
+    // rows that stay open (those that complete a block are in its codes, and nothing reads them from here: the header says how far back a
+    // length may be taken)
     const int64_t open = max(end / kT * kT, old);
     for (int64_t p = tid; p < (end - open) * (DH / 8); p += 256) {
         const int64_t token = open + p / (DH / 8), r = new_row(token);

@@ -349,3 +349,59 @@ def test_tensors_smaller_than_the_shape_are_refused():
     for kw in (dict(v_new=k[:, :1]), dict(n_new=n[:1]), dict(seq_lens=n[:1]), dict(rows=torch.zeros((1, 3), **i32)), dict(n_layers=2)):
         with pytest.raises(ValueError, match=next(iter(kw)) if "n_layers" not in kw else "k_new"):
             ygg.block8_append(s, **{**dict(n_layers=1, k_new=k, v_new=k, cache=one, seq_lens=n, n_new=n), **kw})
+
+
+# ---------------------------------------------------------------- lengths taken back
+
+def _stands_for(cache, b, rows, L, Dh):
+    """Sequence b of a one-layer cache holds the L tokens of rows {"k"/"v": [>= L, Hkv, Dh] float64}."""
+    for x in "kv":
+        codes, scale, tail = (getattr(cache, f"{x}_{y}")[0, b].cpu() for y in ("codes", "scale", "tail"))
+        for k in range(L // 64):
+            block = rows[x][64 * k:64 * k + 64].transpose(1, 0, 2)
+            want = plain.block_scale(block)
+            assert np.array_equal(scale[:, k].numpy(), want), (x, b, L, k)
+            value = plain.decode(codes[:, k].numpy(), want, x)
+            assert (np.abs(value - block) <= np.abs(block) * 2.0 ** -4 + want[:, None, None] * 2.0 ** -10).all(), (x, b, L, k)    # half a step
+        for t in range(L // 64 * 64, L):
+            assert np.array_equal(tail[t % 128].double().numpy(), rows[x][t]), (x, b, L, t)
+
+
+@pytest.mark.parametrize("n", [1, 8, 64, 100, 200])
+def test_lengths_that_may_be_taken_back_to(n):
+    """The open block's tokens, multiples of 64, and in the block before up to where the append that completed it began: attention at each
+    of these lengths, and an append behind it."""
+    Dh, G = 64, 2
+    end = -(-300 // n) * n
+    before = end // 64 - 1                                       # the block before the open one
+    began = (64 * before + 63) // n * n
+    lengths = sorted({*range(64 * (end // 64), end + 1), *range(0, end + 1, 64), *range(64 * before, began + 1)})
+    B = len(lengths)
+    g = np.random.default_rng(n)
+    shape = _shape(B, G, 1, Dh, 1, end + 80)
+    cache = _poisoned(shape, 1)
+    k, v = (_bf16(np.broadcast_to(g.standard_normal((1, 1, end, 1, Dh)), (1, B, end, 1, Dh))) for _ in range(2))
+    i32 = lambda x: torch.full((B,), x, dtype=torch.int32, device=DEV)
+    for at in range(0, end, n):
+        ygg.block8_append(shape, 1, k[:, :, at:at + n].contiguous().to(DEV), v[:, :, at:at + n].contiguous().to(DEV), cache, i32(at + n), i32(n))
+    lens = to_dev(np.array(lengths, np.int32))
+    q, kt, vt = (_bf16(g.standard_normal((B, 1, h, Dh))) for h in (G, 1, 1))
+    out = torch.full((B, 1, G, Dh), float("nan"), dtype=torch.bfloat16, device=DEV)
+    ygg.tree_attention_block8(shape, q.to(DEV), cache.layer(0), lens, kt.to(DEV), vt.to(DEV), i32(-1)[:, None], out, None,
+                              workspace(shape, ygg.OP_ATTENTION_BLOCK8, poison=0xFF))
+    out = to_f64(out)
+    for b, L in enumerate(lengths):
+        _stands_for(cache, b, {"k": k[0, b].double().numpy(), "v": v[0, b].double().numpy()}, L, Dh)
+        dense = {}
+        for x, rows, tree in (("k", k, kt), ("v", v, vt)):
+            blocks = plain.decode(getattr(cache, x + "_codes")[0, b, :, :L // 64].cpu().numpy(), getattr(cache, x + "_scale")[0, b, :, :L // 64].cpu().numpy(), x)
+            dense[x] = np.concatenate((blocks.reshape(-1, Dh), rows[0, b, L // 64 * 64:L, 0].double().numpy(), tree[b, :, 0].double().numpy()))
+        ref, _, size = plain.tree_attention(q[b].double().numpy(), dense["k"], dense["v"], L, np.array([-1]), shape.softmax_scale)
+        # as in _check, with |q|, |k| and |v| below 6: scores off by at most 6 * 6 * 64 * 2^-13 / 8 = 2^-4.8, on both sides of the quotient
+        assert (np.abs(out[b] - ref) <= size * 2 * 2.0 ** -4.8 + 6 * 2.0 ** -12 + np.abs(ref) * 2.0 ** -6).all(), (b, L)
+    more = 70
+    k2, v2 = (_bf16(g.standard_normal((1, B, more, 1, Dh))) for _ in range(2))
+    ygg.block8_append(shape, 1, k2.to(DEV), v2.to(DEV), cache, lens + more, i32(more))
+    for b, L in enumerate(lengths):
+        rows = {x: np.concatenate((old[0, b, :L].double().numpy(), new[0, b].double().numpy())) for x, old, new in (("k", k, k2), ("v", v, v2))}
+        _stands_for(cache, b, rows, L + more, Dh)
