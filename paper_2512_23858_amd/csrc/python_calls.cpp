@@ -83,7 +83,8 @@ struct Args {
         bytes = p ? THPVariable_Unpack(a[i]).nbytes() : 0;
         return p;
     }
-    // A tensor [B, N, ..] whose trailing dimensions are dense and whose B * N rows lie evenly: the row stride in elements
+    // A tensor [B, N, ..] whose trailing dimensions are dense and whose B * N rows lie evenly, each behind the one before: the row
+    // stride in elements (an expanded tensor's stride of 0 would be the calls' word for dense rows, which it does not have)
     void* rows(int i, at::ScalarType want, int64_t& stride, bool any = false) {
         PyObject* o = a[i];
         stride = 0;
@@ -98,7 +99,7 @@ struct Args {
         }
         const int64_t B = t.size(0), N = t.size(1);
         stride = N > 1 ? t.stride(1) : B > 1 ? t.stride(0) : inner;
-        if (B > 1 && N > 1 && t.stride(0) != N * stride) { ok = false; return nullptr; }
+        if ((B > 1 && N > 1 && t.stride(0) != N * stride) || ((B > 1 || N > 1) && stride < inner)) { ok = false; return nullptr; }
         return t.data_ptr();
     }
     // A given tensor has at least so many elements (the kernels go by the shape, not by the tensors)

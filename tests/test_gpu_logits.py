@@ -234,3 +234,18 @@ def test_quotients_at_the_ends_of_the_range_are_the_rounded_ones():
         ref = _ref(h)
     out, best = _run(h)
     assert _same(out, ref) and np.array_equal(best, ref.argmax(-1))
+
+
+@pytest.mark.parametrize("B,N", [(1, 4), (3, 1), (3, 4)])
+def test_expanded_and_overlapping_logits_are_refused(B, N):
+    """One row's memory under several rows: a stride of 0 is no dense tensor."""
+    V = 4096
+    shape, i = _shape(B, N, V), torch.zeros((B, N), dtype=torch.int32, device=DEV)
+    best, ws = torch.full_like(i, -7), workspace(shape, ygg.OP_CONSTRAIN)
+    row = torch.zeros(B * N * V, device=DEV)
+    for x in (row[:V].expand(B, N, V), row.as_strided((B, N, V), (N * (V - 8), V - 8, 1))):
+        with pytest.raises(ValueError, match="rows must be dense"):
+            ygg.constrain_logits(shape, x, i, i, best=best, workspace=ws)
+    assert (best == -7).all()
+    ygg.constrain_logits(shape, row.view(B, N, V), i, i, best=best, workspace=ws)
+    assert (best == 0).all()

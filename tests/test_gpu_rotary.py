@@ -102,3 +102,18 @@ def test_refusals_on_the_gpu_binding():
     for kw in (dict(q=q[:, :3]), dict(q_out=q[:, :3].contiguous()), dict(positions=pos[:, :2].contiguous())):
         with pytest.raises(ValueError, match=next(iter(kw))):
             ygg.tree_rotary(shape, **{**dict(q=q, k=None, q_out=q.clone(), k_out=None, frequencies=f, positions=pos), **kw})
+
+
+@pytest.mark.parametrize("B,N", [(1, 5), (4, 1), (4, 5)])
+def test_expanded_rows_are_refused(B, N):
+    """One token's memory under several tokens: a stride of 0 is no dense tensor."""
+    shape = _shape(B, N, 2, 2, 64, ygg.BF16)
+    one = torch.ones((1, 1, 2, 64), dtype=torch.bfloat16, device=DEV).expand(B, N, 2, 64)
+    full, f, pos = one.contiguous(), ygg.rotary_frequencies(64).to(DEV), torch.zeros((B, N), dtype=torch.int32, device=DEV)
+    out = torch.zeros_like(full)
+    for q, k in ((one, full), (full, one)):
+        with pytest.raises(ValueError, match="rows must be dense"):
+            ygg.tree_rotary(shape, q, k, out, out.clone(), f, positions=pos)
+    assert (out == 0).all()
+    ygg.tree_rotary(shape, full, full, out, out.clone(), f, positions=pos)
+    assert torch.equal(out, full)                                  # position 0
