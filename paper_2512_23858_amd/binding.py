@@ -349,11 +349,15 @@ def _explain_rows(shape, rows, *checks, sizes=()):
 
 
 def _explain_sizes(*sizes):
-    """sizes: (tensor or None, elements that the shape asks for, name); of strided rows, the exact shape instead of a number."""
+    """sizes: (tensor or None, elements that the shape asks for, name); of strided rows, the exact shape instead of a number (a tuple);
+    of rows of several layers, all dimensions, the first as a minimum (a list)."""
     for t, n, name in sizes:
         if t is None:
             continue
-        if isinstance(n, tuple):
+        if isinstance(n, list):
+            if t.dim() != len(n) or t.shape[0] < n[0] or list(t.shape[1:]) != n[1:]:
+                raise ValueError(f"{name}: dimensions {n} are wanted, got {list(t.shape)}")
+        elif isinstance(n, tuple):
             if tuple(t.shape[:2]) != n[:2] or t.numel() != n[0] * n[1] * n[2]:
                 raise ValueError(f"{name}: {n[0]} x {n[1]} rows of {n[2]} elements are wanted, got {tuple(t.shape)}")
         elif t.numel() < n:
@@ -398,10 +402,10 @@ def block8_append(shape: Shape, n_layers: int, k_new, v_new, cache: BlockCache, 
     if rc:
         if rc < 0:
             bf, i32 = torch.bfloat16, torch.int32
-            new = n_layers * shape.batch * (k_new.shape[2] if k_new is not None and k_new.dim() > 2 else 0) * shape.n_kv_heads * shape.head_dim
+            form = [n_layers, shape.batch, k_new.shape[2] if k_new is not None and k_new.dim() > 2 else 0, shape.n_kv_heads, shape.head_dim]
             _explain(shape, (k_new, bf, "k_new"), (v_new, bf, "v_new"), (rows, i32, "rows"), (n_new, i32, "n_new"),
                      (seq_lens, i32, "seq_lens"), *_cache_checks(cache),
-                     sizes=[(k_new, new, "k_new"), (v_new, new, "v_new"), (n_new, shape.batch, "n_new"), (seq_lens, shape.batch, "seq_lens"),
+                     sizes=[(k_new, form, "k_new"), (v_new, form, "v_new"), (n_new, shape.batch, "n_new"), (seq_lens, shape.batch, "seq_lens"),
                             (rows, 0 if rows is None else shape.batch * rows.shape[-1], "rows"), *_cache_sizes(shape, cache, n_layers)])
         _check(rc, "ygg_block8_append")
 

@@ -11,6 +11,9 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <initializer_list>
+
 #include "ygg.h"
 
 namespace {
@@ -111,6 +114,12 @@ struct Args {
         if (!ok || a[i] == Py_None) return;
         const at::Tensor& t = THPVariable_Unpack(a[i]);
         ok = t.size(0) == B && t.size(1) == N && t.numel() == B * N * inner;
+    }
+    // .. and exactly these dimensions behind a first one that is at least `layers`
+    void layers_are(int i, int64_t layers, std::initializer_list<int64_t> behind) {
+        if (!ok || a[i] == Py_None) return;
+        const at::IntArrayRef z = THPVariable_Unpack(a[i]).sizes();
+        ok = z.size() == behind.size() + 1 && z[0] >= layers && std::equal(behind.begin(), behind.end(), z.begin() + 1);
     }
     int32_t size(int i, int64_t d) {   // of a tensor that passed its check, else 0
         if (!ok || a[i] == Py_None) return 0;
@@ -310,7 +319,7 @@ PyObject* block8_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int32_t *rows = t.ints(4), *n_new = t.ints(5), *lens = t.ints(6);
     const ygg_block8_cache c = block_cache(t, 7, s, layers);
     const int32_t n_rows = t.size(2, 2), most = rows ? t.size(4, 1) : n_rows;
-    for (int i : {2, 3}) t.holds(i, (int64_t)layers * s.batch * n_rows * s.n_kv_heads * s.head_dim);
+    for (int i : {2, 3}) t.layers_are(i, layers, {s.batch, n_rows, s.n_kv_heads, s.head_dim});
     t.holds(4, (int64_t)s.batch * most); t.holds(5, s.batch); t.holds(6, s.batch);
     return finish(t.ok, [&](void* st) { return ygg_block8_append(&s, layers, k, v, n_rows, rows, most, n_new, lens, &c, st); });
 }

@@ -405,3 +405,20 @@ def test_lengths_that_may_be_taken_back_to(n):
     for b, L in enumerate(lengths):
         rows = {x: np.concatenate((old[0, b, :L].double().numpy(), new[0, b].double().numpy())) for x, old, new in (("k", k, k2), ("v", v, v2))}
         _stands_for(cache, b, rows, L + more, Dh)
+
+
+def test_new_rows_of_another_form_than_the_cache_are_refused():
+    """Rows without a layer dimension, and K and V of different row counts, hold enough elements but lie differently."""
+    shape = _shape(2, 4, 2, 64, 1, 200)
+    cache, n = _poisoned(shape, 1), torch.tensor([5, 3], dtype=torch.int32, device=DEV)
+    k = torch.ones((1, 2, 5, 2, 64), dtype=torch.bfloat16, device=DEV)
+    call = lambda k_new, v_new, **kw: ygg.block8_append(shape, 1, k_new, v_new, cache, n, n, **kw)
+    for bad in (k[0], k.flatten(3), k.view(1, 2, 5, 1, 128), torch.cat((k, k), 1), torch.cat((k, k), 4)):
+        with pytest.raises(ValueError, match="k_new"):
+            call(bad, bad)
+    for bad in (torch.cat((k, k), 2), k[0], torch.cat((k, k), 1)):
+        with pytest.raises(ValueError, match="v_new"):
+            call(k, bad)
+    assert torch.isnan(cache.k_tail).all() and torch.isnan(cache.v_tail).all()      # nothing was written
+    call(k, k)
+    call(torch.cat((k, k)), k)                                                     # (layers that the call leaves out)
