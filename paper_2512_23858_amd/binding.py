@@ -207,13 +207,15 @@ def _kv_torch_dtype(shape: Shape):
     return {F32: torch.float32, BF16: torch.bfloat16, FP8_E4M3: torch.uint8, FP8_BLOCK: torch.bfloat16}[shape.kv_dtype]
 
 
-def _explain(shape: Shape, *checks, sizes=()):
+def _explain(shape: Shape, *checks, sizes=(), cache=()):
     """The native module refused an argument: run the same checks here, which raise what the caller should see.
-    checks: (tensor or None, wanted dtype or None, name); sizes: as for _explain_sizes."""
+    checks: (tensor or None, wanted dtype or None, name); sizes: as for _explain_sizes; cache: arguments of _explain_cache."""
     shape.c()
     for t, dtype, name in checks:
         _dev(t, dtype, name)
     _explain_sizes(*sizes)
+    if cache:
+        _explain_cache(shape, *cache)
     raise TypeError("an argument is neither a tensor nor None, or a number is out of range")
 
 
@@ -364,10 +366,18 @@ def _explain_sizes(*sizes):
             raise ValueError(f"{name}: {n} elements are wanted, got {t.numel()}")
 
 
-def _cache_sizes(shape: Shape, cache: BlockCache, layers: int):
-    heads, nblk = layers * shape.batch * shape.n_kv_heads, -(-shape.kv_capacity // KV_BLOCK)
-    want = [heads * nblk * KV_BLOCK * shape.head_dim] * 2 + [heads * nblk] * 2 + [heads * 2 * KV_BLOCK * shape.head_dim] * 2
-    return list(zip(cache.tensors(), want, ("k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail")))
+def _explain_cache(shape: Shape, cache: BlockCache, layers: int, alone: bool):
+    """Sizes of a cache's tensors: of `layers` layers (alone: and no more), of the shape's batch and capacity."""
+    B, Hkv, Dh, nblk = shape.batch, shape.n_kv_heads, shape.head_dim, -(-shape.kv_capacity // KV_BLOCK)
+    forms = ((B, Hkv, nblk, KV_BLOCK * Dh), (B, Hkv, nblk), (B, 2 * KV_BLOCK, Hkv, Dh))
+    for i, (t, _, name) in enumerate(_cache_checks(cache)):
+        form = forms[i // 2]
+        per = math.prod(form[1:])
+        if t is None or t.numel() == layers * B * per:
+            continue
+        L, seqs = (t.shape[0], t.shape[1]) if t.dim() == len(form) + 1 else (1, t.shape[0]) if t.dim() == len(form) else (0, 0)
+        if t.numel() != L * seqs * per or (L != 1 if alone else L < layers) or (seqs < B if L == 1 else seqs != B):
+            raise ValueError(f"{name}: {layers} layer{'s' * (layers > 1)} of {list(form)} wanted, got {list(t.shape)}")
 
 
 def _cache_checks(cache: BlockCache):
@@ -386,9 +396,10 @@ def tree_attention_block8(shape: Shape, q, cache: BlockCache, seq_lens, k_tree, 
             _explain(shape, (q, bf, "q"), *_cache_checks(cache), (seq_lens, i32, "seq_lens"), (k_tree, bf, "k_tree"),
                      (v_tree, bf, "v_tree"), (parent_idx, i32, "parent_idx"), (out, bf, "out"), (lse, torch.float32, "lse"),
                      (workspace, None, "workspace"),
-                     sizes=[(q, nodes * q_row, "q"), *_cache_sizes(shape, cache, 1), (seq_lens, shape.batch, "seq_lens"),
+                     sizes=[(q, nodes * q_row, "q"), (seq_lens, shape.batch, "seq_lens"),
                             (k_tree, nodes * kv_row, "k_tree"), (v_tree, nodes * kv_row, "v_tree"), (parent_idx, nodes, "parent_idx"),
-                            (out, nodes * q_row, "out"), (lse, nodes * shape.n_q_heads, "lse")])
+                            (out, nodes * q_row, "out"), (lse, nodes * shape.n_q_heads, "lse")],
+                     cache=(cache, 1, True))
         _check(rc, "ygg_tree_attention_block8")
     return out
 
@@ -406,7 +417,8 @@ def block8_append(shape: Shape, n_layers: int, k_new, v_new, cache: BlockCache, 
             _explain(shape, (k_new, bf, "k_new"), (v_new, bf, "v_new"), (rows, i32, "rows"), (n_new, i32, "n_new"),
                      (seq_lens, i32, "seq_lens"), *_cache_checks(cache),
                      sizes=[(k_new, form, "k_new"), (v_new, form, "v_new"), (n_new, shape.batch, "n_new"), (seq_lens, shape.batch, "seq_lens"),
-                            (rows, 0 if rows is None else shape.batch * rows.shape[-1], "rows"), *_cache_sizes(shape, cache, n_layers)])
+                            (rows, 0 if rows is None else shape.batch * rows.shape[-1], "rows")],
+                     cache=(cache, n_layers, False))
         _check(rc, "ygg_block8_append")
 
 

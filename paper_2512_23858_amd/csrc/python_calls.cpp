@@ -273,18 +273,28 @@ PyObject* accept_and_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// The six tensors of a block cache of so many layers, from argument i on
-ygg_block8_cache block_cache(Args& t, int i, const ygg_shape& s, int64_t layers) {
+// A tensor of a block cache: `per` elements to a sequence in `rank` dimensions, that of the sequences the first, perhaps with a layer
+// dimension before them.  The kernels step by the shape's batch and capacity, so further layers and, behind a single layer, further
+// sequences may follow; a call for one layer takes no tensor of several, which would have to be its first.
+bool cache_part(const at::Tensor& t, int64_t rank, int64_t layers, int64_t batch, int64_t per, bool alone) {
+    if (t.numel() == layers * batch * per) return true;
+    const bool layered = t.dim() == rank + 1;
+    if (!layered && t.dim() != rank) return false;
+    const int64_t L = layered ? t.size(0) : 1, B = t.size(layered ? 1 : 0);
+    return t.numel() == L * B * per && (alone ? L == 1 : L >= layers) && (L == 1 ? B >= batch : B == batch);
+}
+
+// The six tensors of a block cache of so many layers (alone: and no more), from argument i on
+ygg_block8_cache block_cache(Args& t, int i, const ygg_shape& s, int64_t layers, bool alone) {
     ygg_block8_cache c{};
     c.k_codes = t.ptr(i, at::kByte); c.v_codes = t.ptr(i + 1, at::kByte);
     c.k_scale = t.floats(i + 2); c.v_scale = t.floats(i + 3);
     c.k_tail = t.ptr(i + 4, at::kBFloat16); c.v_tail = t.ptr(i + 5, at::kBFloat16);
-    const int64_t heads = layers * s.batch * s.n_kv_heads, nblk = (s.kv_capacity + YGG_KV_BLOCK - 1) / YGG_KV_BLOCK;
-    for (int k = 0; k < 2; ++k) {
-        t.holds(i + k, heads * nblk * YGG_KV_BLOCK * s.head_dim);
-        t.holds(i + 2 + k, heads * nblk);
-        t.holds(i + 4 + k, heads * 2 * YGG_KV_BLOCK * s.head_dim);
-    }
+    const int64_t nblk = (s.kv_capacity + YGG_KV_BLOCK - 1) / YGG_KV_BLOCK, Hkv = s.n_kv_heads;
+    const int64_t per[3] = {Hkv * nblk * YGG_KV_BLOCK * s.head_dim, Hkv * nblk, Hkv * 2 * YGG_KV_BLOCK * s.head_dim}, rank[3] = {4, 3, 4};
+    for (int k = 0; k < 6; ++k)
+        if (t.ok && t.a[i + k] != Py_None)
+            t.ok = cache_part(THPVariable_Unpack(t.a[i + k]), rank[k / 2], layers, s.batch, per[k / 2], alone);
     return c;
 }
 
@@ -294,7 +304,7 @@ PyObject* tree_attention_block8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     ygg_shape s{};
     Args t{a};
     t.ok = read_shape(a[0], s);
-    const ygg_block8_cache c = block_cache(t, 2, s, 1);
+    const ygg_block8_cache c = block_cache(t, 2, s, 1, true);
     void *q = t.ptr(1, at::kBFloat16), *kt = t.ptr(9, at::kBFloat16), *vt = t.ptr(10, at::kBFloat16), *out = t.ptr(12, at::kBFloat16);
     int32_t *lens = t.ints(8), *parent = t.ints(11);
     float* lse = t.floats(13);
@@ -317,7 +327,7 @@ PyObject* block8_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     t.number(1, layers);
     void *k = t.ptr(2, at::kBFloat16), *v = t.ptr(3, at::kBFloat16);
     int32_t *rows = t.ints(4), *n_new = t.ints(5), *lens = t.ints(6);
-    const ygg_block8_cache c = block_cache(t, 7, s, layers);
+    const ygg_block8_cache c = block_cache(t, 7, s, layers, false);
     const int32_t n_rows = t.size(2, 2), most = rows ? t.size(4, 1) : n_rows;
     for (int i : {2, 3}) t.layers_are(i, layers, {s.batch, n_rows, s.n_kv_heads, s.head_dim});
     t.holds(4, (int64_t)s.batch * most); t.holds(5, s.batch); t.holds(6, s.batch);

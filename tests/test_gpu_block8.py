@@ -422,3 +422,26 @@ def test_new_rows_of_another_form_than_the_cache_are_refused():
     assert torch.isnan(cache.k_tail).all() and torch.isnan(cache.v_tail).all()      # nothing was written
     call(k, k)
     call(torch.cat((k, k)), k)                                                     # (layers that the call leaves out)
+
+
+def test_a_cache_of_another_size_is_refused():
+    """Several layers given to the attention of one, a capacity other than the shape's, another batch in several layers."""
+    p = _problem(2, 4, 2, 64, 3, [70, 10], seed=1)
+    s, i32 = p["shape"], dict(dtype=torch.int32, device=DEV)
+    lens = torch.tensor([70, 10], **i32)
+    args = dict(seq_lens=lens, k_tree=p["dense"]["k_tree"], v_tree=p["dense"]["v_tree"], parent_idx=to_dev(p["parent"]), out=torch.empty_like(p["q"]),
+                workspace=workspace(s, ygg.OP_ATTENTION_BLOCK8))
+    wider = ygg.Shape(**{**s.__dict__, "kv_capacity": s.kv_capacity + 128})
+    more = ygg.Shape(**{**s.__dict__, "batch": 4})
+    k, n = torch.zeros((1, 2, 5, 2, 64), dtype=torch.bfloat16, device=DEV), torch.tensor([1, 1], **i32)
+    for cache in (ygg.new_block_cache(s, 2, device=DEV), ygg.new_block_cache(wider, 1, device=DEV), ygg.new_block_cache(more, 2, device=DEV)):
+        with pytest.raises(ValueError, match="k_codes"):
+            ygg.tree_attention_block8(s, p["q"], cache, **args)
+    for cache in (ygg.new_block_cache(wider, 2, device=DEV), ygg.new_block_cache(more, 2, device=DEV), ygg.new_block_cache(s, 1, device=DEV)):
+        with pytest.raises(ValueError, match="k_codes"):
+            ygg.block8_append(s, 2, torch.cat((k, k)), torch.cat((k, k)), cache, n, n)
+    for cache in (ygg.new_block_cache(s, 1, device=DEV), ygg.new_block_cache(more, 1, device=DEV)):     # (further sequences may follow one layer)
+        ygg.tree_attention_block8(s, p["q"], cache, **args)
+        ygg.tree_attention_block8(s, p["q"], cache.layer(0), **args)
+        ygg.block8_append(s, 1, k, k, cache, n, n)
+    ygg.block8_append(s, 1, k, k, ygg.new_block_cache(s, 2, device=DEV), n, n)                          # (and further layers the call's)
