@@ -351,19 +351,22 @@ def _explain_rows(shape, rows, *checks, sizes=()):
 
 
 def _explain_sizes(*sizes):
-    """sizes: (tensor or None, elements that the shape asks for, name); of strided rows, the exact shape instead of a number (a tuple);
-    of rows of several layers, all dimensions, the first as a minimum (a list)."""
+    """sizes: (tensor or None, what the shape asks for, name): a pair, sequences and elements of each (more sequences may follow, and a
+    single one may be longer); three numbers, the exact shape of strided rows; a list, all dimensions, the first as a minimum."""
     for t, n, name in sizes:
         if t is None:
             continue
         if isinstance(n, list):
             if t.dim() != len(n) or t.shape[0] < n[0] or list(t.shape[1:]) != n[1:]:
                 raise ValueError(f"{name}: dimensions {n} are wanted, got {list(t.shape)}")
-        elif isinstance(n, tuple):
+        elif len(n) == 3:
             if tuple(t.shape[:2]) != n[:2] or t.numel() != n[0] * n[1] * n[2]:
                 raise ValueError(f"{name}: {n[0]} x {n[1]} rows of {n[2]} elements are wanted, got {tuple(t.shape)}")
-        elif t.numel() < n:
-            raise ValueError(f"{name}: {n} elements are wanted, got {t.numel()}")
+        else:
+            seqs, per = n
+            if t.numel() != seqs * per and not (seqs == 1 and t.numel() >= per) and not (
+                    t.dim() > 0 and t.shape[0] > seqs and t.numel() == t.shape[0] * per):
+                raise ValueError(f"{name}: {seqs} x {per} elements are wanted, got {tuple(t.shape)}")
 
 
 def _explain_cache(shape: Shape, cache: BlockCache, layers: int, alone: bool):
@@ -392,13 +395,13 @@ def tree_attention_block8(shape: Shape, q, cache: BlockCache, seq_lens, k_tree, 
     if rc:
         if rc < 0:
             bf, i32 = torch.bfloat16, torch.int32
-            nodes, q_row, kv_row = shape.batch * shape.n_nodes, shape.n_q_heads * shape.head_dim, shape.n_kv_heads * shape.head_dim
+            B, N, q_row, kv_row = shape.batch, shape.n_nodes, shape.n_q_heads * shape.head_dim, shape.n_kv_heads * shape.head_dim
             _explain(shape, (q, bf, "q"), *_cache_checks(cache), (seq_lens, i32, "seq_lens"), (k_tree, bf, "k_tree"),
                      (v_tree, bf, "v_tree"), (parent_idx, i32, "parent_idx"), (out, bf, "out"), (lse, torch.float32, "lse"),
                      (workspace, None, "workspace"),
-                     sizes=[(q, nodes * q_row, "q"), (seq_lens, shape.batch, "seq_lens"),
-                            (k_tree, nodes * kv_row, "k_tree"), (v_tree, nodes * kv_row, "v_tree"), (parent_idx, nodes, "parent_idx"),
-                            (out, nodes * q_row, "out"), (lse, nodes * shape.n_q_heads, "lse")],
+                     sizes=[(q, (B, N * q_row), "q"), (seq_lens, (B, 1), "seq_lens"), (k_tree, (B, N * kv_row), "k_tree"),
+                            (v_tree, (B, N * kv_row), "v_tree"), (parent_idx, (B, N), "parent_idx"), (out, (B, N * q_row), "out"),
+                            (lse, (B, N * shape.n_q_heads), "lse")],
                      cache=(cache, 1, True))
         _check(rc, "ygg_tree_attention_block8")
     return out
@@ -416,8 +419,8 @@ def block8_append(shape: Shape, n_layers: int, k_new, v_new, cache: BlockCache, 
             form = [n_layers, shape.batch, k_new.shape[2] if k_new is not None and k_new.dim() > 2 else 0, shape.n_kv_heads, shape.head_dim]
             _explain(shape, (k_new, bf, "k_new"), (v_new, bf, "v_new"), (rows, i32, "rows"), (n_new, i32, "n_new"),
                      (seq_lens, i32, "seq_lens"), *_cache_checks(cache),
-                     sizes=[(k_new, form, "k_new"), (v_new, form, "v_new"), (n_new, shape.batch, "n_new"), (seq_lens, shape.batch, "seq_lens"),
-                            (rows, 0 if rows is None else shape.batch * rows.shape[-1], "rows")],
+                     sizes=[(k_new, form, "k_new"), (v_new, form, "v_new"), (n_new, (shape.batch, 1), "n_new"), (seq_lens, (shape.batch, 1), "seq_lens"),
+                            (rows, (shape.batch, 0 if rows is None else rows.shape[-1]), "rows")],
                      cache=(cache, n_layers, False))
         _check(rc, "ygg_block8_append")
 
@@ -436,9 +439,10 @@ def tree_rotary(shape: Shape, q, k, q_out, k_out, frequencies, seq_lens=None, pa
                           (frequencies, torch.float64, "frequencies"), (seq_lens, i32, "seq_lens"), (parent_idx, i32, "parent_idx"),
                           (positions, i32, "positions"),
                           sizes=[(q, (B, N, shape.n_q_heads * shape.head_dim), "q"), (k, (B, N, shape.n_kv_heads * shape.head_dim), "k"),
-                                 (q_out, B * N * shape.n_q_heads * shape.head_dim, "q_out"),
-                                 (k_out, B * N * shape.n_kv_heads * shape.head_dim, "k_out"), (seq_lens, B, "seq_lens"),
-                                 (parent_idx, B * N, "parent_idx"), (positions, B * N, "positions")])
+                                 (q_out, (B, N * shape.n_q_heads * shape.head_dim), "q_out"),
+                                 (k_out, (B, N * shape.n_kv_heads * shape.head_dim), "k_out"), (positions, (B, N), "positions"),
+                                 (seq_lens if positions is None else None, (B, 1), "seq_lens"),
+                                 (parent_idx if positions is None else None, (B, N), "parent_idx")])
         _check(rc, "ygg_tree_rotary")
 
 
@@ -449,8 +453,8 @@ def count_tokens(shape: Shape, tokens, n_new, counts, rows=None, first: int = 0,
         if rc < 0:
             i32 = torch.int32
             _explain(shape, (tokens, i32, "tokens"), (n_new, i32, "n_new"), (counts, i32, "counts"), (rows, i32, "rows"),
-                     sizes=[(tokens, shape.batch * tokens.shape[-1], "tokens"), (n_new, shape.batch, "n_new"),
-                            (counts, shape.batch * shape.vocab, "counts"), (rows, 0 if rows is None else shape.batch * rows.shape[-1], "rows")])
+                     sizes=[(tokens, (shape.batch, 0 if tokens is None else tokens.shape[-1]), "tokens"), (n_new, (shape.batch, 1), "n_new"),
+                            (counts, (shape.batch, shape.vocab), "counts"), (rows, (shape.batch, 0 if rows is None else rows.shape[-1]), "rows")])
         _check(rc, "ygg_count_tokens")
 
 
@@ -463,18 +467,18 @@ def constrain_logits(shape: Shape, logits, parent_idx, token_ids, out=None, best
     if rc:
         if rc < 0:
             f32, i32 = torch.float32, torch.int32
-            B, V, nodes = shape.batch, shape.vocab, shape.batch * shape.n_nodes
+            B, N, V = shape.batch, shape.n_nodes, shape.vocab
             if logits is not None and logits.dtype not in (f32, torch.bfloat16):
                 raise TypeError(f"logits: expected {f32} or {torch.bfloat16}, got {logits.dtype}")
             _explain_rows(shape, ((logits, None, "logits"),), (parent_idx, i32, "parent_idx"), (token_ids, i32, "token_ids"),
                           (out, f32, "out"), (best, i32, "best"), (counts, i32, "counts"), (repetition, f32, "repetition"),
                           (presence, f32, "presence"), (frequency, f32, "frequency"), (bias, f32, "bias"), (masks, i32, "masks"),
                           (mask_index, i32, "mask_index"), (workspace, None, "workspace"),
-                          sizes=[(logits, (B, shape.n_nodes, V), "logits"), (parent_idx, nodes, "parent_idx"), (token_ids, nodes, "token_ids"),
-                                 (out, nodes * V, "out"), (best, nodes, "best"), (counts, B * V, "counts"), (repetition, B, "repetition"),
-                                 (presence, B, "presence"), (frequency, B, "frequency"),
-                                 (bias, V if bias is not None and bias.dim() == 1 else B * V, "bias"),
-                                 (masks, 0 if masks is None else masks.shape[0] * (-(-V // 32)), "masks"), (mask_index, nodes, "mask_index")])
+                          sizes=[(logits, (B, N, V), "logits"), (parent_idx, (B, N), "parent_idx"), (token_ids, (B, N), "token_ids"),
+                                 (out, (B, N * V), "out"), (best, (B, N), "best"), (counts, (B, V), "counts"), (repetition, (B, 1), "repetition"),
+                                 (presence, (B, 1), "presence"), (frequency, (B, 1), "frequency"),
+                                 (bias, (1 if bias is not None and bias.dim() == 1 else B, V), "bias"),
+                                 (masks, (0 if masks is None else masks.shape[0], -(-V // 32)), "masks"), (mask_index, (B, N), "mask_index")])
         _check(rc, "ygg_constrain_logits")
 
 

@@ -105,9 +105,13 @@ struct Args {
         if ((B > 1 && N > 1 && t.stride(0) != N * stride) || ((B > 1 || N > 1) && stride < inner)) { ok = false; return nullptr; }
         return t.data_ptr();
     }
-    // A given tensor has at least so many elements (the kernels go by the shape, not by the tensors)
-    void holds(int i, int64_t n) {
-        if (ok && a[i] != Py_None && THPVariable_Unpack(a[i]).numel() < n) ok = false;
+    // A given tensor has `per` elements to a sequence (the kernels go by the shape, not by the tensors).  More sequences may follow,
+    // and a single one may be longer: where several are, the next one would not begin where the kernels step to.
+    void holds(int i, int64_t seqs, int64_t per) {
+        if (!ok || a[i] == Py_None) return;
+        const at::Tensor& t = THPVariable_Unpack(a[i]);
+        const int64_t n = t.numel();
+        ok = n == seqs * per || (seqs == 1 && n >= per) || (t.dim() > 0 && t.size(0) > seqs && n == t.size(0) * per);
     }
     // .. and these leading dimensions, with `inner` elements behind them
     void rows_are(int i, int64_t B, int64_t N, int64_t inner) {
@@ -310,10 +314,10 @@ PyObject* tree_attention_block8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     float* lse = t.floats(13);
     size_t wn;
     void* ws = t.scratch(14, wn);
-    const int64_t nodes = (int64_t)s.batch * s.n_nodes;
-    for (int i : {1, 12}) t.holds(i, nodes * s.n_q_heads * s.head_dim);
-    for (int i : {9, 10}) t.holds(i, nodes * s.n_kv_heads * s.head_dim);
-    t.holds(8, s.batch); t.holds(11, nodes); t.holds(13, nodes * s.n_q_heads);
+    const int64_t B = s.batch, N = s.n_nodes;
+    for (int i : {1, 12}) t.holds(i, B, N * s.n_q_heads * s.head_dim);
+    for (int i : {9, 10}) t.holds(i, B, N * s.n_kv_heads * s.head_dim);
+    t.holds(8, B, 1); t.holds(11, B, N); t.holds(13, B, N * s.n_q_heads);
     return finish(t.ok, [&](void* st) { return ygg_tree_attention_block8(&s, q, &c, lens, kt, vt, parent, out, lse, ws, wn, st); });
 }
 
@@ -330,7 +334,7 @@ PyObject* block8_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const ygg_block8_cache c = block_cache(t, 7, s, layers, false);
     const int32_t n_rows = t.size(2, 2), most = rows ? t.size(4, 1) : n_rows;
     for (int i : {2, 3}) t.layers_are(i, layers, {s.batch, n_rows, s.n_kv_heads, s.head_dim});
-    t.holds(4, (int64_t)s.batch * most); t.holds(5, s.batch); t.holds(6, s.batch);
+    t.holds(4, s.batch, most); t.holds(5, s.batch, 1); t.holds(6, s.batch, 1);
     return finish(t.ok, [&](void* st) { return ygg_block8_append(&s, layers, k, v, n_rows, rows, most, n_new, lens, &c, st); });
 }
 
@@ -348,7 +352,8 @@ PyObject* tree_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int32_t *lens = t.ints(6), *parent = t.ints(7), *positions = t.ints(8);
     const int64_t B = s.batch, N = s.n_nodes, q_row = (int64_t)s.n_q_heads * s.head_dim, k_row = (int64_t)s.n_kv_heads * s.head_dim;
     t.rows_are(1, B, N, q_row); t.rows_are(2, B, N, k_row);
-    t.holds(3, B * N * q_row); t.holds(4, B * N * k_row); t.holds(6, B); t.holds(7, B * N); t.holds(8, B * N);
+    t.holds(3, B, N * q_row); t.holds(4, B, N * k_row); t.holds(8, B, N);
+    if (!positions) { t.holds(6, B, 1); t.holds(7, B, N); }   // (else they are not read)
     const bool interleaved = a[9] == Py_True;
     const double scale = PyFloat_AsDouble(a[10]);
     if (PyErr_Occurred()) { PyErr_Clear(); t.ok = false; }
@@ -367,7 +372,7 @@ PyObject* count_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int32_t first = 0;
     t.number(5, first);
     const int32_t n_tokens = t.size(1, 1), most = rows ? t.size(4, 1) : n_tokens;
-    t.holds(1, (int64_t)s.batch * n_tokens); t.holds(2, s.batch); t.holds(3, (int64_t)s.batch * s.vocab); t.holds(4, (int64_t)s.batch * most);
+    t.holds(1, s.batch, n_tokens); t.holds(2, s.batch, 1); t.holds(3, s.batch, s.vocab); t.holds(4, s.batch, most);
     const bool prompt = a[6] == Py_True;
     return finish(t.ok, [&](void* st) { return ygg_count_tokens(&s, tokens, n_tokens, rows, first, most, n_new, prompt, counts, st); });
 }
@@ -395,11 +400,11 @@ PyObject* constrain_logits(PyObject*, PyObject* const* a, Py_ssize_t n) {
     r.masks = reinterpret_cast<const uint32_t*>(t.ints(11));
     r.n_masks = t.size(11, 0);
     r.mask_index = t.ints(12);
-    const int64_t B = s.batch, nodes = B * s.n_nodes, V = s.vocab;
-    t.rows_are(1, B, s.n_nodes, V);
-    for (int i : {2, 3, 5, 12}) t.holds(i, nodes);
-    for (int i : {7, 8, 9}) t.holds(i, B);
-    t.holds(4, nodes * V); t.holds(6, B * V); t.holds(10, r.bias_shared ? V : B * V); t.holds(11, r.n_masks * ((V + 31) / 32));
+    const int64_t B = s.batch, N = s.n_nodes, V = s.vocab;
+    t.rows_are(1, B, N, V);
+    for (int i : {2, 3, 5, 12}) t.holds(i, B, N);
+    for (int i : {7, 8, 9}) t.holds(i, B, 1);
+    t.holds(4, B, N * V); t.holds(6, B, V); t.holds(10, r.bias_shared ? 1 : B, V); t.holds(11, r.n_masks, (V + 31) / 32);
     size_t wn;
     void* ws = t.scratch(13, wn);
     return finish(t.ok, [&](void* st) { return ygg_constrain_logits(&s, x, dt, stride, parent, token, &r, out, best, ws, wn, st); });

@@ -445,3 +445,20 @@ def test_a_cache_of_another_size_is_refused():
         ygg.tree_attention_block8(s, p["q"], cache.layer(0), **args)
         ygg.block8_append(s, 1, k, k, cache, n, n)
     ygg.block8_append(s, 1, k, k, ygg.new_block_cache(s, 2, device=DEV), n, n)                          # (and further layers the call's)
+
+
+def test_longer_trees_than_the_shape_are_refused_in_a_batch():
+    p = _problem(2, 4, 2, 64, 3, [70, 10], seed=1)
+    s = p["shape"]
+    good = dict(q=p["q"], seq_lens=torch.tensor([70, 10], dtype=torch.int32, device=DEV), k_tree=p["dense"]["k_tree"], v_tree=p["dense"]["v_tree"],
+                parent_idx=to_dev(p["parent"]), out=torch.empty_like(p["q"]), lse=torch.empty((2, 3, 4), device=DEV))
+    ws = workspace(s, ygg.OP_ATTENTION_BLOCK8)
+    for name in ("q", "k_tree", "v_tree", "parent_idx", "out", "lse"):
+        with pytest.raises(ValueError, match=name):
+            ygg.tree_attention_block8(s, cache=p["cache"], workspace=ws, **{**good, name: torch.cat((good[name], good[name]), 1)})
+    # one sequence: the first nodes of a longer tree
+    first = ygg.Shape(**{**s.__dict__, "n_nodes": 2, "batch": 1})
+    out = torch.full_like(p["q"], float("nan"))
+    ygg.tree_attention_block8(first, cache=p["cache"], workspace=ws, **{**good, "out": out[:1], "lse": None, **{x: good[x][:1] for x in (
+        "q", "k_tree", "v_tree", "parent_idx")}})
+    assert not torch.isnan(out[0, :2]).any() and torch.isnan(out[0, 2:]).all() and torch.isnan(out[1]).all()

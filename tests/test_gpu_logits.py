@@ -249,3 +249,29 @@ def test_expanded_and_overlapping_logits_are_refused(B, N):
     assert (best == -7).all()
     ygg.constrain_logits(shape, row.view(B, N, V), i, i, best=best, workspace=ws)
     assert (best == 0).all()
+
+
+def test_tensors_with_longer_rows_than_the_shape_are_refused():
+    """Counts, biases, masks or an output of a padded vocabulary have enough elements, but the second row lies elsewhere."""
+    shape = _shape(2, 3, 100)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    good = dict(logits=torch.zeros((2, 3, 100), device=DEV), parent_idx=torch.full((2, 3), -1, **i32), token_ids=torch.zeros((2, 3), **i32),
+                out=torch.zeros((2, 3, 100), device=DEV), best=torch.zeros((2, 3), **i32), counts=torch.zeros((2, 100), **i32),
+                bias=torch.zeros((2, 100), device=DEV), masks=torch.full((2, 4), -1, **i32), mask_index=torch.zeros((2, 3), **i32),
+                workspace=workspace(shape, ygg.OP_CONSTRAIN))
+    ygg.constrain_logits(shape, **good)
+    for name in ("parent_idx", "token_ids", "out", "best", "counts", "bias", "masks", "mask_index"):
+        t = good[name]
+        with pytest.raises(ValueError, match=name):
+            ygg.constrain_logits(shape, **{**good, name: torch.cat((t, t), -1)})
+        if name != "masks":                                        # further sequences may follow, and further masks
+            ygg.constrain_logits(shape, **{**good, name: torch.cat((t, t), 0)})
+    t, n = torch.zeros((2, 7), **i32), torch.ones(2, **i32)
+    wide = torch.zeros((2, 128), **i32)
+    with pytest.raises(ValueError, match="counts"):
+        ygg.count_tokens(shape, t, n, wide)
+    assert not wide.any()
+    # a single sequence may be the first part of a longer one
+    one = _shape(1, 3, 100)
+    ygg.constrain_logits(one, good["logits"][:1], torch.full((1, 9), -1, **i32), torch.zeros((1, 9), **i32), best=good["best"], counts=wide[:1],
+                         workspace=good["workspace"])
