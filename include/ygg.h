@@ -308,7 +308,8 @@ typedef struct {
 
 /*
  * Tree attention (see ygg_tree_attention) of one layer over such a cache; shape->kv_dtype == YGG_FP8_BLOCK, head_dim 64 or 128.
- * A tree of one node (n_nodes 1, depth 0) is plain decoding.  The keys and values of cache and tree must be finite.
+ * A tree of one node (n_nodes 1, depth 0) is plain decoding.  q and the keys and values of cache and tree must be finite, below 2^60 in
+ * magnitude, with scores softmax_scale * q.k below 2^23 in magnitude (fp32, to 2^-24 of a score).
  *   q, out [B,N,Hq,Dh] bf16;  k_tree, v_tree [B,N,Hkv,Dh] bf16;  lse [B,N,Hq] fp32 or NULL;  seq_lens, parent_idx int32
  * q (bf16, 8 bits of significand) and the softmax weights enter the products as sums of two E4M3 values, that is with 8 bits and
  * an exponent per row and tile; softmax and accumulation are fp32 (the matrix instructions of 8-bit values cut each product at

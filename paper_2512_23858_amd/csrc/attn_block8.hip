@@ -62,13 +62,14 @@ struct Layout {
 };
 
 // What a workgroup accumulates for its rows: 2^ref * O~ and 2^ref * l.  A lane holds row n = lane % 32 of its wavefront's block; ref is
-// a whole number, the same in both halves of the wavefront, and l is that half's share.
+// a whole number, the same in both halves of the wavefront, and l is that half's share.  A row that has seen no key yet has no reference
+// (any is false, and its sums are zero): no number serves for one, since scores may lie as far below it.
 template <int DH>
 struct Rows {
     f32x16 o[DH / 32];
     int ref;
     float l;
-    bool any;       // (wave-uniform) some key was seen: ref is set
+    bool any;       // some key was seen: ref is set
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int d = 0; d < DH / 32; ++d) o[d] = f32x16{};
@@ -297,10 +298,10 @@ __device__ __forceinline__ void own_keys(unsigned char* smem, Rows<DH>& x, int b
             top = fmaxf(top, s[e]);
         }
         top = other_half_max(top);
-        // a row that sees none of the tile's keys keeps its reference; before it has one, any serves
-        const int c = top == -INFINITY ? (x.any ? x.ref : -(1 << 20)) : (int)ceilf(top);
+        const bool some = top != -INFINITY;                 // a row that sees none of the tile's keys stays as it is
+        const int c = some ? (int)ceilf(top) : x.ref;
         if (!x.any) x.ref = c;
-        x.any = true;
+        x.any |= some;
         x.refer_to(c);
         const float off = (float)x.ref;
         float p[16];
