@@ -430,6 +430,14 @@ int32_t ygg_debug_attention_plan(const ygg_shape *shape, int32_t *plan /* [5], h
 int32_t ygg_debug_attention_launch(const ygg_shape *shape, int32_t *launch /* [3], host */);
 
 /*
+ * The launch plan of ygg_tree_attention_block8 for a shape (host only): plan[0] = 32-row blocks to a workgroup, plan[1] = such
+ * workgroups along the query rows of one kv head, plan[2] = row blocks of the workgroups of the rows beyond them (0: none),
+ * plan[3] and plan[4] = equal runs that either kind cuts the batch's keys into (0: a workgroup to each sequence), plan[5] = 1 if a
+ * workgroup has twice the wavefronts, plan[6] = lanes to a row in the merge of partial results (0: no merge).
+ */
+int32_t ygg_debug_block8_plan(const ygg_shape *shape, int32_t *plan /* [7], host */);
+
+/*
  * Tuning hook: forces the workgroup shape (wavefronts, 32-row blocks per wavefront, key shares) and/or the number
  * of key splits of every later ygg_tree_attention call of this process; a field left 0 keeps the library's own
  * choice, an unknown shape is ignored, and (0, 0, 0, 0) removes the override.  The workspace must be sized

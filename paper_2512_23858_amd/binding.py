@@ -125,6 +125,8 @@ def load_library() -> ctypes.CDLL:
         lib.ygg_debug_attention_plan.argtypes = [shp, ctypes.POINTER(i32)]
         lib.ygg_debug_attention_launch.restype = i32
         lib.ygg_debug_attention_launch.argtypes = [shp, ctypes.POINTER(i32)]
+        lib.ygg_debug_block8_plan.restype = i32
+        lib.ygg_debug_block8_plan.argtypes = [shp, ctypes.POINTER(i32)]
         lib.ygg_debug_tree_attention_main.restype = i32
         lib.ygg_debug_tree_attention_main.argtypes = [shp] + [vp] * 9 + [vp, sz, vp]
         _lib = lib
@@ -496,6 +498,14 @@ def attention_launch(shape: Shape) -> dict:
     out = (ctypes.c_int32 * 3)()
     _check(load_library().ygg_debug_attention_launch(ctypes.byref(cs), out), "ygg_debug_attention_launch")
     return dict(opposite_phases=bool(out[0]), tree_cost=out[1], lds_bytes=out[2])
+
+
+def block8_plan(shape: Shape) -> dict:
+    """ygg_debug_block8_plan: the launch plan of tree_attention_block8 for this shape (host only)."""
+    cs = shape.c()
+    out = (ctypes.c_int32 * 7)()
+    _check(load_library().ygg_debug_block8_plan(ctypes.byref(cs), out), "ygg_debug_block8_plan")
+    return dict(row_blocks=out[0], row_tiles=out[1], rem_blocks=out[2], runs=out[3], rem_runs=out[4], wide=bool(out[5]), merge_lanes=out[6])
 
 
 def init():

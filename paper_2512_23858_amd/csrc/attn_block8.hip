@@ -673,7 +673,7 @@ hipError_t raise() {
 }
 
 template <int DH, int NW, int RB, int REM>
-hipError_t launch(Block8Args a, hipStream_t st) {
+hipError_t launch(Block8Args a, int merge_lanes, hipStream_t st) {
     size_t smem = Layout<DH, NW, RB>::smem(a.N);
     if constexpr (REM > 0) smem = std::max(smem, Layout<DH, NW, REM>::smem(a.N));
     if (smem > kAttnMfmaMaxSmem) return hipErrorInvalidValue;
@@ -686,11 +686,10 @@ hipError_t launch(Block8Args a, hipStream_t st) {
         if (kOneReader<RB> || a.row_tiles == 1) hipLaunchKernelGGL((attn_block8_kernel<DH, NW, RB, REM, true>), grid, dim3(NW * 64), smem, st, a);
     if constexpr (!kOneReader<RB>)
         if (kManyReaders<REM> || a.row_tiles > 1) hipLaunchKernelGGL((attn_block8_kernel<DH, NW, RB, REM, false>), grid, dim3(NW * 64), smem, st, a);
-    if (const hipError_t e = hipGetLastError(); e != hipSuccess || (a.runs <= 1 && a.rem_runs <= 1)) return e;   // (no sequence is cut)
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess || merge_lanes == 0) return e;
     constexpr int LPR = DH / 8;
     auto groups = [&](int lanes) { return dim3((unsigned)(((int64_t)a.N * a.Hq * lanes + 255) / 256), (unsigned)a.B); };
-    // few rows: a whole wavefront to each
-    if (a.rows_total <= 4096) hipLaunchKernelGGL((block8_merge_kernel<DH, 64 / LPR>), groups(64), dim3(256), 0, st, a);
+    if (merge_lanes == 64) hipLaunchKernelGGL((block8_merge_kernel<DH, 64 / LPR>), groups(64), dim3(256), 0, st, a);
     else hipLaunchKernelGGL((block8_merge_kernel<DH, 1>), groups(LPR), dim3(256), 0, st, a);
     return hipGetLastError();
 }
@@ -698,12 +697,12 @@ hipError_t launch(Block8Args a, hipStream_t st) {
 template <int DH>
 hipError_t launch_for(const Block8Args& a, const Block8Plan& p, hipStream_t st) {
     switch (p.row_blocks * 10 + p.rem_blocks) {
-        case 10: return p.wide ? launch<DH, 4, 1, 0>(a, st) : launch<DH, 2, 1, 0>(a, st);
-        case 20: return p.wide ? launch<DH, 8, 2, 0>(a, st) : launch<DH, 4, 2, 0>(a, st);
-        case 40: return p.wide ? launch<DH, 8, 4, 0>(a, st) : launch<DH, 4, 4, 0>(a, st);
-        case 80: return launch<DH, 8, 8, 0>(a, st);
-        case 82: return launch<DH, 8, 8, 2>(a, st);
-        case 84: return launch<DH, 8, 8, 4>(a, st);
+        case 10: return p.wide ? launch<DH, 4, 1, 0>(a, p.merge_lanes, st) : launch<DH, 2, 1, 0>(a, p.merge_lanes, st);
+        case 20: return p.wide ? launch<DH, 8, 2, 0>(a, p.merge_lanes, st) : launch<DH, 4, 2, 0>(a, p.merge_lanes, st);
+        case 40: return p.wide ? launch<DH, 8, 4, 0>(a, p.merge_lanes, st) : launch<DH, 4, 4, 0>(a, p.merge_lanes, st);
+        case 80: return launch<DH, 8, 8, 0>(a, p.merge_lanes, st);
+        case 82: return launch<DH, 8, 8, 2>(a, p.merge_lanes, st);
+        case 84: return launch<DH, 8, 8, 4>(a, p.merge_lanes, st);
         default: return hipErrorInvalidValue;
     }
 }

@@ -329,6 +329,8 @@ Block8Plan plan_block8(const ygg_shape& s) {
         p.wide = groups <= 256 && p.row_blocks < 8 && s.max_seq_len / YGG_KV_BLOCK >= 4;
     }
     const int32_t nsplit = std::max({p.runs, p.rem_runs, 1});
+    // few rows: a whole wavefront to each in the merge
+    p.merge_lanes = nsplit == 1 ? 0 : (int64_t)s.batch * s.n_nodes * s.n_q_heads <= 4096 ? 64 : s.head_dim / 8;
     p.part_o_bytes = part_o_bytes(s, true, nsplit);
     p.part_rec_bytes = part_rec_bytes(s, nsplit);
     p.seq_splits_bytes = align256(2 * (size_t)s.batch * sizeof(int32_t));
@@ -385,6 +387,15 @@ int32_t ygg_debug_attention_launch(const ygg_shape* s, int32_t* launch) {
     const AttnPlan p = plan_attention(*s);
     launch[0] = p.phases; launch[1] = p.tree_cost;
     launch[2] = p.use_mfma ? (int32_t)attn_mfma_smem(p.waves, p.kshares, s->head_dim, s->n_q_heads / s->n_kv_heads, s->n_nodes) : 0;
+    return YGG_OK;
+}
+
+int32_t ygg_debug_block8_plan(const ygg_shape* s, int32_t* plan) {
+    if (int32_t rc = check_block8(s)) return rc;
+    if (!plan) return YGG_ERR_NULL;
+    const Block8Plan p = plan_block8(*s);
+    plan[0] = p.row_blocks; plan[1] = p.row_tiles; plan[2] = p.rem_blocks; plan[3] = p.runs; plan[4] = p.rem_runs;
+    plan[5] = p.wide; plan[6] = p.merge_lanes;
     return YGG_OK;
 }
 

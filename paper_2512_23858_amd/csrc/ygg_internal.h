@@ -165,6 +165,7 @@ struct Block8Plan {
     int32_t runs, rem_runs;   // equal runs of the batch's keys per (kv head, row tile), one workgroup each, at most 64; 0: one to a sequence
     int32_t most_runs;    // the most that this or a shorter bound on the lengths may take
     int32_t lead, own;    // what a segment costs beside its keys, in blocks, and the tiles of a sequence's own keys
+    int32_t merge_lanes;  // lanes to a row of the merge of partials: a wavefront's or as many as hold the row once; 0: no sequence is cut
     size_t part_o_bytes, part_rec_bytes, seq_splits_bytes;
 };
 struct Block8Args {
