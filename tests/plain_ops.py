@@ -102,3 +102,16 @@ def constrain(logits, parent, token, counts, repetition, presence, frequency, bi
                 x = np.where((words[v // 32] >> (v % 32).astype(np.uint32)) & 1, x, f32(-np.inf))
             out[i] = x
     return out
+
+
+def encode(x, scale, which):
+    """Bytes of a block in storage order, [.., 64*Dh] uint8, of rows x [.., 64, Dh] at fp32 scales [..]: the E4M3 value nearest to
+    x * (1 / scale) in fp32, ties to even."""
+    y = x.astype(np.float32) * (np.float32(1) / scale.astype(np.float32))[..., None, None]
+    size = np.abs(y).astype(np.float64)
+    step = np.exp2(np.maximum(np.frexp(size)[1] - 1, -6) - 3.0)
+    code = np.searchsorted(e4m3_values()[:127], np.minimum(np.rint(size / step) * step, 448.0))      # (rint: ties to even)
+    code = (code | np.where(np.signbit(y), 128, 0)).astype(np.uint8)
+    out = np.empty((*x.shape[:-2], 64 * x.shape[-1]), np.uint8)
+    out[..., stored_at(which, x.shape[-1])] = code
+    return out

@@ -462,3 +462,35 @@ def test_longer_trees_than_the_shape_are_refused_in_a_batch():
     ygg.tree_attention_block8(first, cache=p["cache"], workspace=ws, **{**good, "out": out[:1], "lse": None, **{x: good[x][:1] for x in (
         "q", "k_tree", "v_tree", "parent_idx")}})
     assert not torch.isnan(out[0, :2]).any() and torch.isnan(out[0, 2:]).all() and torch.isnan(out[1]).all()
+
+
+@pytest.mark.parametrize("Dh", [64, 128])
+def test_codes_are_the_ones_of_the_definition_byte_for_byte(Dh):
+    """Random blocks of many sizes, values half way between two codes at a scale of a power of two (ties), zeros of both signs, steps
+    below the smallest normal code, and largest magnitudes whose quotient rounds above 448."""
+    Hkv, blocks = 3, 40
+    g = np.random.default_rng(Dh)
+    shape = _shape(1, Hkv, Hkv, Dh, 1, 64 * blocks)
+    cache = _poisoned(shape, 1)
+    x = g.standard_normal((2, blocks, 64, Hkv, Dh)) * np.exp2(g.integers(-12, 12, (2, blocks, 1, Hkv, 1)))
+    values = plain.e4m3_values()[:127]
+    ties = np.concatenate(((values[1:] + values[:-1]) / 2, values))
+    x[:, 3:9] = g.choice(np.concatenate((ties, -ties)), (2, 6, 64, Hkv, Dh))
+    x[:, 3:9, 0, :, 0] = 448.0
+    x[:, 5] *= 2.0 ** -7
+    x[:, 6] *= 2.0 ** 30
+    x[:, 9:12, ::3] = -0.0
+    x[:, 10, 1::3] *= 1e-4
+    rows = _bf16(x.reshape(2, 1, 1, blocks * 64, Hkv, Dh))
+    n = torch.tensor([64 * blocks], dtype=torch.int32, device=DEV)
+    ygg.block8_append(shape, 1, rows[0].to(DEV), rows[1].to(DEV), cache, n, n)
+    for i, which in enumerate("kv"):
+        block = rows[i].double().numpy().reshape(blocks, 64, Hkv, Dh).transpose(2, 0, 1, 3)          # [Hkv, blocks, 64, Dh]
+        scale = plain.block_scale(block)
+        assert np.array_equal(getattr(cache, which + "_scale")[0, 0].cpu().numpy(), scale)
+        got, want = getattr(cache, which + "_codes")[0, 0].cpu().numpy(), plain.encode(block, scale, which)
+        assert np.array_equal(got, want), (which, np.argwhere(got != want)[:5])
+        # the test does reach ties, and they go both ways
+        tied = np.isin(np.abs(block[:, 3]), (values[1:] + values[:-1]) / 2)
+        kept = np.abs(plain.decode(want[:, 3], np.ones(Hkv, np.float32), which)) > np.abs(block[:, 3])
+        assert (tied & kept).any() and (tied & ~kept).any() and (scale[:, 3] == 1).all()

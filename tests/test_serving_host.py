@@ -212,3 +212,14 @@ def test_public_names_of_the_header_are_in_the_package():
     header = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "ygg.h")).read(), flags=re.S)
     for name in ("ygg_tree_attention_block8", "ygg_block8_append", "ygg_tree_rotary", "ygg_count_tokens", "ygg_constrain_logits"):
         assert re.search(rf"\b{name}\s*\(", header) and hasattr(ygg.load_library(), name) and callable(getattr(ygg, name[4:]))
+
+
+def test_the_definition_of_the_codes_is_the_nearest_value():
+    """plain_ops.encode against torch's rounding to E4M3, and back through the storage order."""
+    g = np.random.default_rng(0)
+    values = plain.e4m3_values()[:127]
+    x = np.concatenate((values, (values[1:] + values[:-1]) / 2, g.standard_normal(64 * 128 - 253) * np.exp2(g.integers(-12, 8, 64 * 128 - 253))))
+    x = np.clip(np.where(g.random(x.size) < 0.5, x, -x), -448, 448).astype(np.float32).reshape(1, 64, 128)
+    for which in "kv":
+        code = plain.encode(x, np.ones(1, np.float32), which)[:, plain.stored_at(which, 128)]
+        assert np.array_equal(code, torch.from_numpy(x).to(torch.float8_e4m3fn).view(torch.uint8).numpy())
