@@ -306,7 +306,7 @@ __device__ __forceinline__ void own_keys(unsigned char* smem, Rows<DH>& x, int b
         const float off = (float)x.ref;
         float p[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
+        for (int e = 0; e < 16; ++e) {   // the sum is the log-sum-exp's too, so it takes the weights before they are rounded for the product
             p[e] = __builtin_amdgcn_exp2f(s[e] - off);
             x.l += p[e];
         }

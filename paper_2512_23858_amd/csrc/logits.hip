@@ -5,9 +5,10 @@
 //                     with its confirmed count, path count, bias and mask bit.  The arithmetic is fp32, one rounding per step as
 //                     the definition has it (no fused multiply-add), so that equal inputs give equal ties.
 //   best_kernel       the chunks' maxima of a row, first maximum.
-// Bound by the stream of logits in and out; counts and biases of a sequence are read by all of its nodes and stay in L2.  129 rows of
+// Counts and biases of a sequence are read by all of its nodes and stay in L2.  129 rows of
 // 128256 bf16 logits with everything on: 25.3 us with both kernels (a copy of their size takes 18), 784 rows of 32003 fp32 logits read for
-// their maxima only 31.6.  Many resident wavefronts with few registers serve best: four rows to a workgroup that share counts and biases, or
+// their maxima only 31.9.  Both are bound by vector instructions: 42 to 44 per logit, with which the SIMDs are busy all the time
+// (counted).  Many resident wavefronts with few registers serve best: four rows to a workgroup that share counts and biases, or
 // all of a thread's loads up front, or penalties for listed tokens only, measured 41 to 60 us.  The logits are stored past the caches: with
 // plain stores 35 us instead of 25, though a reader that follows at once (an argmax over them) then ends 3 us earlier (50.7 and 53.7 us
 // for both).

@@ -313,10 +313,14 @@ Block8Plan plan_block8(const ygg_shape& s) {
         p.most_runs = (int32_t)std::max({runs, rem, (int64_t)p.most_runs});
     }
     // A workgroup to each sequence where that ends sooner than runs and their merge (4.5 us).  Units take 0.5, 0.6, 1.0 and 1.8 us for one,
-    // two, four and eight row blocks where a workgroup has its compute unit to itself, and a little over half of that at head_dim 64.  It is
-    // no later either where all sequences at their bound take memory longer than the longest takes its workgroup (8 x 4096 tokens on 32 kv
-    // heads 72 -> 68 us, from 2000 to 4096 tokens 58 -> 52, 400 to 4096 49 -> 48), up to 4096 tokens or so: of 700 to 8192 the longest ends
-    // at 89 us and runs at 74.
+    // two, four and eight row blocks where a workgroup has its compute unit to itself, and a little over half of that at head_dim 64.  Runs
+    // are priced by the same units, without the second workgroup of a compute unit and without memory, so too low where these count: 9, 24
+    // and 28 us for 3 x 2047 tokens of 65 nodes (measured 17.5), one token of 16 requests (35), 49 nodes of 8 x 4096 on 32 kv heads (64).
+    // The second clause makes up for that where all sequences at their bound take memory longer than the longest takes its workgroup, for
+    // bounds up to somewhere between 4096 and 8192 tokens (of 700 to 8192 the longest ends at 89 us and runs at 74).  Lengths are on the
+    // device, and the even batch is the one that gains: runs -> a workgroup to each, 49 nodes, 8 sequences on 32 kv heads of 4096 tokens
+    // each 64 -> 60 us, from 512 to 4096 47 -> 48, one of 4096 among seven of 128 31 -> 44.  A program whose bound is far above most
+    // lengths does better with a bound beyond these.
     const float unit = (p.row_blocks == 1 ? 0.5f : p.row_blocks == 2 ? 0.6f : p.row_blocks == 4 ? 1.0f : 1.8f) * (s.head_dim == 64 ? 0.6f : 1.f);
     const int64_t groups = (int64_t)s.batch * Hkv * (p.row_tiles + (p.rem_blocks ? 1 : 0));
     const int64_t rounds = (groups + slots - 1) / slots;
