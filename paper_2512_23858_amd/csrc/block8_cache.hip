@@ -7,7 +7,7 @@
 // tokens, transposes them in registers to words of four tokens, and the words meet in LDS (gathered there byte by byte they took half
 // as many instructions again as all the rest).  The workgroup of the first touched block also copies the rows that stay open to the
 // tail, after it has read that block's old rows: they may lie in the same half of it.  Bound by the stream of rows: 8191 tokens of four
-// layers and 8 kv heads of 128 45.4 us, 4.4 TB/s of rows and codes; the accepted tokens of 16 requests in 32 layers 16.4 us, most of its
+// layers and 8 kv heads of 128 45.4 us, 4.4 TB/s of rows and codes; the accepted tokens of 16 requests in 32 layers 14 to 16 us, most of its
 // bytes being the rows of completed blocks.
 #include "ygg_internal.h"
 #include "ygg_device.h"
