@@ -425,12 +425,12 @@ def _encode_k(x):
 
 
 def _encode_v(x):
-    """V of whole blocks: 32 dimensions after another, tokens in the order in which the scores of a 32 x 32 matrix instruction lie in its
-    accumulator; the 32 tokens of a lane share a scale."""
+    """V of whole blocks: 32 dimensions after another, 32 tokens to a lane in the order in which a matrix instruction meets the scores of
+    another one's accumulator."""
     Dh = x.shape[-1]
     x = x.reshape(*x.shape[:-2], 2, 4, 2, 4, Dh // 32, 32)                                     # tokens: u e4 h e1   dimensions: d r
     n = x.dim() - 6
-    x = x.permute(*range(n), n + 4, n + 2, n + 5, n, n + 1, n + 3)                             # d h r, u e4 e1
+    x = x.permute(*range(n), n + 4, n, n + 5, n + 2, n + 1, n + 3)                             # d u r, h e4 e1
     codes, scale = _encode(x.reshape(*x.shape[:n + 3], 32))
     return codes.reshape(*x.shape[:n], 32 * Dh), scale.permute(*range(n), n + 1, n + 2, n).reshape(*x.shape[:n], 2 * Dh)
 
@@ -484,7 +484,7 @@ def _plain_attend(s):
     K = _decoded(s["k_codes"].view(B, Hkv, nblk, 2, J, 2, 32, 16), s["k_scale"].view(B, Hkv, nblk, 2, 32, 2, J).permute(0, 1, 2, 5, 6, 3, 4))
     K = K.permute(0, 1, 2, 3, 6, 4, 5, 7).reshape(B, Hkv, -1, Dh)                              # t r, j h i
     V = _decoded(s["v_codes"].view(B, Hkv, nblk, Dh // 32, 2, 32, 16), s["v_scale"].view(B, Hkv, nblk, 2, 32, Dh // 32).permute(0, 1, 2, 5, 3, 4))
-    V = V.view(B, Hkv, nblk, Dh // 32, 2, 32, 2, 4, 4).permute(0, 1, 2, 6, 7, 4, 8, 3, 5).reshape(B, Hkv, -1, Dh)      # u e4 h e1, d r
+    V = V.view(B, Hkv, nblk, Dh // 32, 2, 32, 2, 4, 4).permute(0, 1, 2, 4, 7, 6, 8, 3, 5).reshape(B, Hkv, -1, Dh)      # u e4 h e1, d r
     seq, r = torch.arange(B, device=DEV)[:, None], torch.arange(BLOCK, device=DEV)
     half = (full % (2 * BLOCK))[:, None] + r
     K = torch.cat((K, s["k_tail"][seq, half].float().transpose(1, 2), s["k_tree"].float().transpose(1, 2)), 2)
@@ -620,7 +620,7 @@ def _stored_at(case, which):
     if which == "k":
         chunk, lane, i = t // 32 * (Dh // 64) + d // 64, d // 32 % 2 * 32 + t % 32, d % 32
     else:
-        chunk, lane, i = d // 32, t // 4 % 2 * 32 + d % 32, t // 32 * 16 + t % 32 // 8 * 4 + t % 4
+        chunk, lane, i = d // 32, t // 32 * 32 + d % 32, t // 4 % 2 * 16 + t % 32 // 8 * 4 + t % 4
     return torch.from_numpy(chunk * 2048 + lane * 32 + i).to(DEV), torch.from_numpy(lane * (Dh // 32) + chunk).to(DEV)
 
 
