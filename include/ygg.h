@@ -21,6 +21,13 @@
  *   ygg_constrain_logits      penalties, biases and grammar masks on logits, node by node, and their first maxima
  *   ygg_count_tokens          the counts of confirmed tokens that the penalties go by
  *
+ * A prompt's way into the cache, and a cache in 4 bits:
+ *
+ *   ygg_tree_norm_rotary      RMS norms of every head of the queries and keys and their rotary positions, in one pass
+ *   ygg_prompt_attention      causal attention of whole prompts, or of the next chunk of them, sequences of different lengths
+ *   ygg_block4_append         writes accepted (or prompt) tokens into a cache in 4 bits with a scale per 32 values
+ *   ygg_tree_attention_block4 the verifier's attention (or plain decoding) over that cache
+ *
  * Conventions shared by every call
  *   - All tensor pointers are DEVICE pointers owned by the caller; the ygg_shape struct is HOST
  *     memory and is only read during the call.  The library never allocates, frees or keeps
@@ -71,14 +78,17 @@ typedef enum {
     YGG_BF16 = 1,
     YGG_FP8_E4M3 = 2,  /* K and V (cache and tree) as 8-bit E4M3 codes, Q and O bf16; head_dim 128;
                           accepted by ygg_tree_attention_fp8kv and ygg_accept_and_compact only */
-    YGG_FP8_BLOCK = 3  /* the cache is a ygg_block8_cache, everything else is bf16; accepted by
+    YGG_FP8_BLOCK = 3, /* the cache is a ygg_block8_cache, everything else is bf16; accepted by
                           ygg_tree_attention_block8, ygg_block8_append and ygg_tree_rotary, and by
                           ygg_accept_and_compact with n_layers = 0 */
+    YGG_FP4_BLOCK = 5  /* the cache is a ygg_block4_cache, everything else is bf16; accepted by ygg_tree_attention_block4,
+                          ygg_block4_append, ygg_tree_norm_rotary and ygg_tree_rotary, and by ygg_accept_and_compact with
+                          n_layers = 0 (4 is no type) */
 } ygg_dtype;
 
 typedef enum {
     YGG_OP_ATTENTION = 0, YGG_OP_EXPAND = 1, YGG_OP_ACCEPT = 2, YGG_OP_ATTACH = 3,
-    YGG_OP_ATTENTION_BLOCK8 = 4, YGG_OP_CONSTRAIN = 5
+    YGG_OP_ATTENTION_BLOCK8 = 4, YGG_OP_CONSTRAIN = 5, YGG_OP_ATTENTION_BLOCK4 = 6, YGG_OP_PROMPT_ATTENTION = 7
 } ygg_op;
 
 typedef struct {
@@ -354,6 +364,78 @@ int32_t ygg_tree_rotary(const ygg_shape *shape, const void *q, int64_t q_stride,
                         void *hip_stream);
 
 /*
+ * The same rotation behind a norm of every head, in one pass over q and k: with x a head's values of one token and w its weights,
+ *     y_d = x_d * w_d / sqrt(sum_d x_d^2 / head_dim + eps)   in fp32, not rounded; then the pairs of y as above, rounded once
+ *   q_weight, k_weight [Dh] fp32 device, or [Hq,Dh] and [Hkv,Dh] if weights_per_head, 16-byte aligned; needed with their tensor
+ *   eps          finite, >= 0.  (A head of zeros is 0 also with eps = 0.)  The sum of the squares must stay below fp32's largest value
+ * Everything else as for ygg_tree_rotary.
+ */
+int32_t ygg_tree_norm_rotary(const ygg_shape *shape, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                             void *q_out, void *k_out, const float *q_weight, const float *k_weight, int32_t weights_per_head,
+                             float eps, const double *frequencies, int32_t rotary_dim, int32_t interleaved, float scale,
+                             const int32_t *seq_lens, const int32_t *parent_idx, const int32_t *positions, void *hip_stream);
+
+/*
+ * Causal attention of whole prompts, or of the next chunk of them behind keys that are cached already, for one layer.  Sequence b has
+ * its queries in rows q_first[b] .. + q_len[b] - 1 of q and out, and its keys in rows k_first[b] .. + k_len[b] - 1 of k and v: packed
+ * sequences, padded ones and slabs of a cache [B,cap,Hkv,Dh] (k_first[b] = b * cap) alike.  The last query sees every key:
+ *     keys J(i) = { j : j <= i + k_len[b] - q_len[b] }   for query i of sequence b, i = 0 .. q_len[b] - 1
+ *     out[q_first[b]+i,h,:] = sum_j softmax_j(softmax_scale * q_i . k_j[g,:]) * v_j[g,:],  lse = ln sum_j exp(softmax_scale * q_i . k_j)
+ * A query that sees no key (q_len > k_len) gets zeros, and -inf as lse.  Scores, softmax and accumulation are fp32; with bf16 the softmax
+ * weights are rounded to bf16 for the value product.
+ *
+ *   shape        kv_dtype YGG_F32 or YGG_BF16; batch = sequences; n_nodes = rows of q and out, those of all sequences together (any
+ *                number up to 2^25); kv_capacity = rows of k and v; max_seq_len = a bound of k_len, at most kv_capacity; depth, width
+ *                and vocab are not read
+ *   q, out [n_nodes,Hq,Dh];  k, v [kv_capacity,Hkv,Dh];  lse [n_nodes,Hq] fp32 or NULL.  Rows of q, k and v are q_stride, k_stride and
+ *                v_stride elements apart (0: dense), so that parts of a fused projection can be given; out is dense and overlaps nothing
+ *   q_first, q_len, k_first, k_len [B] int32 device.  No two sequences share rows of q; they may share keys.  A sequence that does not
+ *                lie inside the rows is cut to those that do, and k_len to max_seq_len.  Rows of out and lse of no sequence are not written
+ * Workspace: ygg_workspace_bytes(PROMPT_ATTENTION), which may be 0; what serves max_seq_len serves every smaller one.
+ */
+int32_t ygg_prompt_attention(const ygg_shape *shape, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                             const void *v, int64_t v_stride, const int32_t *q_first, const int32_t *q_len,
+                             const int32_t *k_first, const int32_t *k_len, void *out, float *lse,
+                             void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * A K/V cache in 4 bits.  Blocks, tails, lengths and what a length can be taken back to are those of ygg_block8_cache; a block holds
+ * E2M1 codes (1 sign, 2 exponent bits, 1 of significand: 0, 0.5, 1, 1.5, 2, 3, 4, 6) two to a byte, the even one in the low half, with
+ * a power of two to 32 values: of K to the 32 dimensions 32i .. 32i+31 of a token, of V to the 32 tokens 32i .. 32i+31 of the block of a
+ * dimension, which are the groups that gfx950's matrix instructions scale by themselves.  A stored element is 2^(scale - 127) * value(code).
+ *
+ *   k_codes, v_codes [B,Hkv,nblk,32*Dh] bytes;  k_scale, v_scale [B,Hkv,nblk,2*Dh] bytes, 27 .. 253 (2^-100 .. 2^126)
+ *   k_tail, v_tail   [B,128,Hkv,Dh] bf16;  all 16-byte aligned
+ * Inside a block, with token t and dimension d, the code is number 2048*chunk + 32*lane + e and the scale byte lane*(Dh/32) + chunk:
+ *   K: chunk = t/32*(Dh/64) + d/64,  lane = 32*(d/32%2) + t%32,  e = d%32
+ *   V: chunk = d/32,                 lane = 32*(t/32) + d%32,    e = 16*(t/4%2) + 4*(t%32/8) + t%4
+ */
+typedef struct {
+    void *k_codes, *v_codes;
+    void *k_scale, *v_scale;
+    void *k_tail, *v_tail;
+} ygg_block4_cache;
+
+/*
+ * Tree attention (see ygg_tree_attention) of one layer over such a cache; shape->kv_dtype == YGG_FP4_BLOCK.  Everything else as for
+ * ygg_tree_attention_block8, the ranges of values and the two E4M3 values for each of q and the weights included.
+ * Workspace: ygg_workspace_bytes(ATTENTION_BLOCK4).
+ */
+int32_t ygg_tree_attention_block4(const ygg_shape *shape, const void *q, const ygg_block4_cache *cache /* host struct */,
+                                  const int32_t *seq_lens, const void *k_tree, const void *v_tree,
+                                  const int32_t *parent_idx, void *out, float *lse,
+                                  void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Appends new tokens to such a cache, all layers in one launch.  Arguments are those of ygg_block8_append.  A block that is completed
+ * is encoded: the scale of 32 values is the least 2^e, e >= -100, with max|x| <= 7 * 2^e, and a code the nearest to x / 2^e, ties to the
+ * even code, what lies beyond 6 as 6 (values between 6 and 7 are off by no more than those between 4 and 6 may be).
+ */
+int32_t ygg_block4_append(const ygg_shape *shape, int32_t n_layers, const void *k_new, const void *v_new, int32_t n_rows,
+                          const int32_t *rows, int32_t max_new, const int32_t *n_new, const int32_t *seq_lens,
+                          const ygg_block4_cache *cache /* host struct */, void *hip_stream);
+
+/*
  * Adds tokens to the counts that ygg_constrain_logits goes by.
  *   tokens [B,n_tokens] int32;  rows [B,max_new] int32 or NULL: the k-th token added is tokens[b][rows[b][k]], or tokens[b][first+k]
  *   n_new  [B] int32: tokens to add, 0 .. max_new (clamped to that);  prompt != 0: marks them as the prompt's instead of counting
@@ -436,6 +518,14 @@ int32_t ygg_debug_attention_launch(const ygg_shape *shape, int32_t *launch /* [3
  * workgroup has twice the wavefronts, plan[6] = lanes to a row in the merge of partial results (0: no merge).
  */
 int32_t ygg_debug_block8_plan(const ygg_shape *shape, int32_t *plan /* [7], host */);
+/* .. and that of ygg_tree_attention_block4, likewise. */
+int32_t ygg_debug_block4_plan(const ygg_shape *shape, int32_t *plan /* [7], host */);
+
+/*
+ * The launch plan of ygg_prompt_attention for a shape (host only): plan[0] = rows (queries x heads of a group) to a workgroup, plan[1] =
+ * parts into which a workgroup's keys are split, plan[2] = row tiles that the batch can have per kv head.
+ */
+int32_t ygg_debug_prompt_plan(const ygg_shape *shape, int32_t *plan /* [3], host */);
 
 /*
  * Tuning hook: forces the workgroup shape (wavefronts, 32-row blocks per wavefront, key shares) and/or the number

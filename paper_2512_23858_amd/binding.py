@@ -17,8 +17,9 @@ import torch
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 OP_ATTENTION, OP_EXPAND, OP_ACCEPT, OP_ATTACH, OP_ATTENTION_BLOCK8, OP_CONSTRAIN = 0, 1, 2, 3, 4, 5
-F32, BF16, FP8_E4M3, FP8_BLOCK = 0, 1, 2, 3
-KV_BLOCK = 64      # tokens to a block of the 8-bit block cache
+OP_ATTENTION_BLOCK4, OP_PROMPT_ATTENTION = 6, 7
+F32, BF16, FP8_E4M3, FP8_BLOCK, FP4_BLOCK = 0, 1, 2, 3, 5
+KV_BLOCK = 64      # tokens to a block of the 8-bit and of the 4-bit block cache
 
 
 class _CShape(ctypes.Structure):
@@ -68,7 +69,13 @@ class BlockCache:
 
     def layer(self, i: int) -> "BlockCache":
         """Views of one layer."""
-        return BlockCache(*(t[i] for t in self.tensors()))
+        return type(self)(*(t[i] for t in self.tensors()))
+
+
+@dataclass
+class Block4Cache(BlockCache):
+    """The tensors of a 4-bit block cache (ygg_block4_cache in include/ygg.h), of one layer or with a leading layer dimension:
+    codes [B,Hkv,nblk,32*Dh] uint8 (two to a byte), scales [B,Hkv,nblk,2*Dh] uint8 (exponents + 127), tails [B,128,Hkv,Dh] bf16."""
 
 
 _lib = None
@@ -114,6 +121,11 @@ def load_library() -> ctypes.CDLL:
         for name, args in (("ygg_tree_attention_block8", [shp] + [vp] * 8 + [vp, sz, vp]),
                            ("ygg_block8_append", [shp, i32, vp, vp, i32, vp, i32, vp, vp, vp, vp]),
                            ("ygg_tree_rotary", [shp, vp, ctypes.c_int64, vp, ctypes.c_int64] + [vp] * 3 + [i32, i32, ctypes.c_float] + [vp] * 4),
+                           ("ygg_tree_attention_block4", [shp] + [vp] * 8 + [vp, sz, vp]),
+                           ("ygg_block4_append", [shp, i32, vp, vp, i32, vp, i32, vp, vp, vp, vp]),
+                           ("ygg_tree_norm_rotary", [shp, vp, ctypes.c_int64, vp, ctypes.c_int64] + [vp] * 4 +
+                            [i32, ctypes.c_float, vp, i32, i32, ctypes.c_float] + [vp] * 4),
+                           ("ygg_prompt_attention", [shp] + [vp, ctypes.c_int64] * 3 + [vp] * 6 + [vp, sz, vp]),
                            ("ygg_count_tokens", [shp, vp, i32, vp, i32, i32, vp, i32, vp, vp]),
                            ("ygg_constrain_logits", [shp, vp, i32, ctypes.c_int64] + [vp] * 5 + [vp, sz, vp])):
             getattr(lib, name).restype, getattr(lib, name).argtypes = i32, args
@@ -125,8 +137,8 @@ def load_library() -> ctypes.CDLL:
         lib.ygg_debug_attention_plan.argtypes = [shp, ctypes.POINTER(i32)]
         lib.ygg_debug_attention_launch.restype = i32
         lib.ygg_debug_attention_launch.argtypes = [shp, ctypes.POINTER(i32)]
-        lib.ygg_debug_block8_plan.restype = i32
-        lib.ygg_debug_block8_plan.argtypes = [shp, ctypes.POINTER(i32)]
+        for name in ("ygg_debug_block8_plan", "ygg_debug_block4_plan", "ygg_debug_prompt_plan"):
+            getattr(lib, name).restype, getattr(lib, name).argtypes = i32, [shp, ctypes.POINTER(i32)]
         lib.ygg_debug_tree_attention_main.restype = i32
         lib.ygg_debug_tree_attention_main.argtypes = [shp] + [vp] * 9 + [vp, sz, vp]
         _lib = lib
@@ -173,6 +185,16 @@ def new_block_cache(shape: Shape, n_layers: int = 1, device="cuda:0") -> BlockCa
                       *(torch.zeros(tails, dtype=torch.bfloat16, device=device) for _ in range(2)))
 
 
+def new_block4_cache(shape: Shape, n_layers: int = 1, device="cuda:0") -> Block4Cache:
+    """Allocates an empty 4-bit block cache of n_layers layers through torch (zeros, at scales of 1)."""
+    if workspace_bytes(shape, OP_ATTENTION_BLOCK4) == 0:
+        raise ValueError("invalid shape for a 4-bit block cache")
+    codes, scales, tails = ((n_layers, *form) for form in _cache_forms(shape, Block4Cache))
+    return Block4Cache(*(torch.zeros(codes, dtype=torch.uint8, device=device) for _ in range(2)),
+                       *(torch.full(scales, 127, dtype=torch.uint8, device=device) for _ in range(2)),
+                       *(torch.zeros(tails, dtype=torch.bfloat16, device=device) for _ in range(2)))
+
+
 def rotary_frequencies(rotary_dim: int, base: float = 10000.0, factor: float = 1.0, original_len: int = 0,
                        low_turns: float = 1.0, high_turns: float = 4.0) -> torch.Tensor:
     """Frequency table [rotary_dim/2] of tree_rotary on the host, fp64: base^(-2j/rotary_dim) radians per position.
@@ -206,7 +228,8 @@ def _check(rc: int, what: str):
 
 def _kv_torch_dtype(shape: Shape):
     """Element type of the K/V tensors (8-bit codes travel as uint8)."""
-    return {F32: torch.float32, BF16: torch.bfloat16, FP8_E4M3: torch.uint8, FP8_BLOCK: torch.bfloat16}[shape.kv_dtype]
+    return {F32: torch.float32, BF16: torch.bfloat16, FP8_E4M3: torch.uint8, FP8_BLOCK: torch.bfloat16,
+            FP4_BLOCK: torch.bfloat16}[shape.kv_dtype]
 
 
 def _explain(shape: Shape, *checks, sizes=(), cache=()):
@@ -371,10 +394,17 @@ def _explain_sizes(*sizes):
                 raise ValueError(f"{name}: {seqs} x {per} elements are wanted, got {tuple(t.shape)}")
 
 
+def _cache_forms(shape: Shape, kind):
+    """Dimensions of one layer's codes, scales and tails."""
+    B, Hkv, Dh, nblk = shape.batch, shape.n_kv_heads, shape.head_dim, -(-shape.kv_capacity // KV_BLOCK)
+    if kind is Block4Cache:
+        return (B, Hkv, nblk, KV_BLOCK * Dh // 2), (B, Hkv, nblk, 2 * Dh), (B, 2 * KV_BLOCK, Hkv, Dh)
+    return (B, Hkv, nblk, KV_BLOCK * Dh), (B, Hkv, nblk), (B, 2 * KV_BLOCK, Hkv, Dh)
+
+
 def _explain_cache(shape: Shape, cache: BlockCache, layers: int, alone: bool):
     """Sizes of a cache's tensors: of `layers` layers (alone: and no more), of the shape's batch and capacity."""
-    B, Hkv, Dh, nblk = shape.batch, shape.n_kv_heads, shape.head_dim, -(-shape.kv_capacity // KV_BLOCK)
-    forms = ((B, Hkv, nblk, KV_BLOCK * Dh), (B, Hkv, nblk), (B, 2 * KV_BLOCK, Hkv, Dh))
+    B, forms = shape.batch, _cache_forms(shape, type(cache))
     for i, (t, _, name) in enumerate(_cache_checks(cache)):
         form = forms[i // 2]
         per = math.prod(form[1:])
@@ -386,8 +416,21 @@ def _explain_cache(shape: Shape, cache: BlockCache, layers: int, alone: bool):
 
 
 def _cache_checks(cache: BlockCache):
-    want = (torch.uint8, torch.uint8, torch.float32, torch.float32, torch.bfloat16, torch.bfloat16)
+    scale = torch.uint8 if isinstance(cache, Block4Cache) else torch.float32
+    want = (torch.uint8, torch.uint8, scale, scale, torch.bfloat16, torch.bfloat16)
     return list(zip(cache.tensors(), want, ("k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail")))
+
+
+def _explain_attention_block(shape, q, cache, seq_lens, k_tree, v_tree, parent_idx, out, lse, workspace):
+    bf, i32 = torch.bfloat16, torch.int32
+    B, N, q_row, kv_row = shape.batch, shape.n_nodes, shape.n_q_heads * shape.head_dim, shape.n_kv_heads * shape.head_dim
+    _explain(shape, (q, bf, "q"), *_cache_checks(cache), (seq_lens, i32, "seq_lens"), (k_tree, bf, "k_tree"),
+             (v_tree, bf, "v_tree"), (parent_idx, i32, "parent_idx"), (out, bf, "out"), (lse, torch.float32, "lse"),
+             (workspace, None, "workspace"),
+             sizes=[(q, (B, N * q_row), "q"), (seq_lens, (B, 1), "seq_lens"), (k_tree, (B, N * kv_row), "k_tree"),
+                    (v_tree, (B, N * kv_row), "v_tree"), (parent_idx, (B, N), "parent_idx"), (out, (B, N * q_row), "out"),
+                    (lse, (B, N * shape.n_q_heads), "lse")],
+             cache=(cache, 1, True))
 
 
 def tree_attention_block8(shape: Shape, q, cache: BlockCache, seq_lens, k_tree, v_tree, parent_idx, out, lse=None, workspace=None):
@@ -396,17 +439,30 @@ def tree_attention_block8(shape: Shape, q, cache: BlockCache, seq_lens, k_tree, 
                                                      cache.v_tail, seq_lens, k_tree, v_tree, parent_idx, out, lse, workspace)
     if rc:
         if rc < 0:
-            bf, i32 = torch.bfloat16, torch.int32
-            B, N, q_row, kv_row = shape.batch, shape.n_nodes, shape.n_q_heads * shape.head_dim, shape.n_kv_heads * shape.head_dim
-            _explain(shape, (q, bf, "q"), *_cache_checks(cache), (seq_lens, i32, "seq_lens"), (k_tree, bf, "k_tree"),
-                     (v_tree, bf, "v_tree"), (parent_idx, i32, "parent_idx"), (out, bf, "out"), (lse, torch.float32, "lse"),
-                     (workspace, None, "workspace"),
-                     sizes=[(q, (B, N * q_row), "q"), (seq_lens, (B, 1), "seq_lens"), (k_tree, (B, N * kv_row), "k_tree"),
-                            (v_tree, (B, N * kv_row), "v_tree"), (parent_idx, (B, N), "parent_idx"), (out, (B, N * q_row), "out"),
-                            (lse, (B, N * shape.n_q_heads), "lse")],
-                     cache=(cache, 1, True))
+            _explain_attention_block(shape, q, cache, seq_lens, k_tree, v_tree, parent_idx, out, lse, workspace)
         _check(rc, "ygg_tree_attention_block8")
     return out
+
+
+def tree_attention_block4(shape: Shape, q, cache: Block4Cache, seq_lens, k_tree, v_tree, parent_idx, out, lse=None, workspace=None):
+    """ygg_tree_attention_block4: tree attention of one layer over a 4-bit block cache (shape.kv_dtype FP4_BLOCK)."""
+    rc = (_native or _calls()).tree_attention_block4(shape, q, cache.k_codes, cache.v_codes, cache.k_scale, cache.v_scale, cache.k_tail,
+                                                     cache.v_tail, seq_lens, k_tree, v_tree, parent_idx, out, lse, workspace)
+    if rc:
+        if rc < 0:
+            _explain_attention_block(shape, q, cache, seq_lens, k_tree, v_tree, parent_idx, out, lse, workspace)
+        _check(rc, "ygg_tree_attention_block4")
+    return out
+
+
+def _explain_append(shape, n_layers, k_new, v_new, cache, seq_lens, n_new, rows):
+    bf, i32 = torch.bfloat16, torch.int32
+    form = [n_layers, shape.batch, k_new.shape[2] if k_new is not None and k_new.dim() > 2 else 0, shape.n_kv_heads, shape.head_dim]
+    _explain(shape, (k_new, bf, "k_new"), (v_new, bf, "v_new"), (rows, i32, "rows"), (n_new, i32, "n_new"),
+             (seq_lens, i32, "seq_lens"), *_cache_checks(cache),
+             sizes=[(k_new, form, "k_new"), (v_new, form, "v_new"), (n_new, (shape.batch, 1), "n_new"), (seq_lens, (shape.batch, 1), "seq_lens"),
+                    (rows, (shape.batch, 0 if rows is None else rows.shape[-1]), "rows")],
+             cache=(cache, n_layers, False))
 
 
 def block8_append(shape: Shape, n_layers: int, k_new, v_new, cache: BlockCache, seq_lens, n_new, rows=None):
@@ -417,14 +473,18 @@ def block8_append(shape: Shape, n_layers: int, k_new, v_new, cache: BlockCache, 
                                              cache.k_scale, cache.v_scale, cache.k_tail, cache.v_tail)
     if rc:
         if rc < 0:
-            bf, i32 = torch.bfloat16, torch.int32
-            form = [n_layers, shape.batch, k_new.shape[2] if k_new is not None and k_new.dim() > 2 else 0, shape.n_kv_heads, shape.head_dim]
-            _explain(shape, (k_new, bf, "k_new"), (v_new, bf, "v_new"), (rows, i32, "rows"), (n_new, i32, "n_new"),
-                     (seq_lens, i32, "seq_lens"), *_cache_checks(cache),
-                     sizes=[(k_new, form, "k_new"), (v_new, form, "v_new"), (n_new, (shape.batch, 1), "n_new"), (seq_lens, (shape.batch, 1), "seq_lens"),
-                            (rows, (shape.batch, 0 if rows is None else rows.shape[-1]), "rows")],
-                     cache=(cache, n_layers, False))
+            _explain_append(shape, n_layers, k_new, v_new, cache, seq_lens, n_new, rows)
         _check(rc, "ygg_block8_append")
+
+
+def block4_append(shape: Shape, n_layers: int, k_new, v_new, cache: Block4Cache, seq_lens, n_new, rows=None):
+    """ygg_block4_append: the same into a 4-bit block cache."""
+    rc = (_native or _calls()).block4_append(shape, n_layers, k_new, v_new, rows, n_new, seq_lens, cache.k_codes, cache.v_codes,
+                                             cache.k_scale, cache.v_scale, cache.k_tail, cache.v_tail)
+    if rc:
+        if rc < 0:
+            _explain_append(shape, n_layers, k_new, v_new, cache, seq_lens, n_new, rows)
+        _check(rc, "ygg_block4_append")
 
 
 def tree_rotary(shape: Shape, q, k, q_out, k_out, frequencies, seq_lens=None, parent_idx=None, positions=None, interleaved: bool = False,
@@ -446,6 +506,58 @@ def tree_rotary(shape: Shape, q, k, q_out, k_out, frequencies, seq_lens=None, pa
                                  (seq_lens if positions is None else None, (B, 1), "seq_lens"),
                                  (parent_idx if positions is None else None, (B, N), "parent_idx")])
         _check(rc, "ygg_tree_rotary")
+
+
+def tree_norm_rotary(shape: Shape, q, k, q_out, k_out, q_weight, k_weight, frequencies, seq_lens=None, parent_idx=None, positions=None,
+                     interleaved: bool = False, scale: float = 1.0, eps: float = 1e-6):
+    """ygg_tree_norm_rotary: RMS norm of every head of q and k with the weights (fp32, [Dh], or [Hq,Dh] and [Hkv,Dh]), then the rotation of
+    tree_rotary, in one pass."""
+    rc = (_native or _calls()).tree_norm_rotary(shape, q, k, q_out, k_out, q_weight, k_weight, frequencies, seq_lens, parent_idx, positions,
+                                                True if interleaved else False, scale, eps)
+    if rc:
+        if rc < 0:
+            dt, i32, f32 = torch.float32 if shape.kv_dtype == F32 else torch.bfloat16, torch.int32, torch.float32
+            B, N, Hq, Hkv, Dh = shape.batch, shape.n_nodes, shape.n_q_heads, shape.n_kv_heads, shape.head_dim
+            own = any(w is not None and w.dim() == 2 for w in (q_weight, k_weight))
+            for w, heads, name in ((q_weight, Hq, "q_weight"), (k_weight, Hkv, "k_weight")):
+                if w is not None and tuple(w.shape) != ((heads, Dh) if own else (Dh,)):
+                    raise ValueError(f"{name}: {[heads, Dh] if own else [Dh]} is wanted (as the other's), got {list(w.shape)}")
+            _explain_rows(shape, ((q, dt, "q"), (k, dt, "k")), (q_out, dt, "q_out"), (k_out, dt, "k_out"), (q_weight, f32, "q_weight"),
+                          (k_weight, f32, "k_weight"), (frequencies, torch.float64, "frequencies"), (seq_lens, i32, "seq_lens"),
+                          (parent_idx, i32, "parent_idx"), (positions, i32, "positions"),
+                          sizes=[(q, (B, N, Hq * Dh), "q"), (k, (B, N, Hkv * Dh), "k"), (q_out, (B, N * Hq * Dh), "q_out"),
+                                 (k_out, (B, N * Hkv * Dh), "k_out"), (positions, (B, N), "positions"),
+                                 (seq_lens if positions is None else None, (B, 1), "seq_lens"),
+                                 (parent_idx if positions is None else None, (B, N), "parent_idx")])
+        _check(rc, "ygg_tree_norm_rotary")
+
+
+def prompt_attention(shape: Shape, q, k, v, q_first, q_len, k_first, k_len, out, lse=None, workspace=None):
+    """ygg_prompt_attention: causal attention of sequences whose queries are rows q_first .. + q_len - 1 of q [n_nodes,Hq,Dh] and whose
+    keys are rows k_first .. + k_len - 1 of k and v [kv_capacity,Hkv,Dh] (rows may be strided); the last query sees every key.
+    shape.max_seq_len bounds k_len."""
+    rc = (_native or _calls()).prompt_attention(shape, q, k, v, q_first, q_len, k_first, k_len, out, lse, workspace)
+    if rc:
+        if rc < 0:
+            dt, i32 = torch.float32 if shape.kv_dtype == F32 else torch.bfloat16, torch.int32
+            q_row, k_row, cap = shape.n_q_heads * shape.head_dim, shape.n_kv_heads * shape.head_dim, shape.kv_capacity
+            for t, rows, inner, name in ((q, shape.n_nodes, q_row, "q"), (k, cap, k_row, "k"), (v, cap, k_row, "v")):
+                if t is None:
+                    continue
+                if not t.is_cuda:
+                    raise ValueError(f"{name} must be a GPU tensor")
+                if t.dtype != dt:
+                    raise TypeError(f"{name}: expected {dt}, got {t.dtype}")
+                if t.dim() < 2 or t.shape[0] != rows or t.numel() != rows * inner:
+                    raise ValueError(f"{name}: {rows} rows of {inner} elements are wanted, got {tuple(t.shape)}")
+                if not t[0].is_contiguous() or (rows > 1 and t.stride(0) < inner):
+                    raise ValueError(f"{name}: rows must be dense and lie evenly")
+            _explain(shape, (q_first, i32, "q_first"), (q_len, i32, "q_len"), (k_first, i32, "k_first"), (k_len, i32, "k_len"), (out, dt, "out"),
+                     (lse, torch.float32, "lse"), (workspace, None, "workspace"),
+                     sizes=[(t, (shape.batch, 1), name) for t, name in ((q_first, "q_first"), (q_len, "q_len"), (k_first, "k_first"), (k_len, "k_len"))] +
+                           [(out, (1, shape.n_nodes * q_row), "out"), (lse, (1, shape.n_nodes * shape.n_q_heads), "lse")])
+        _check(rc, "ygg_prompt_attention")
+    return out
 
 
 def count_tokens(shape: Shape, tokens, n_new, counts, rows=None, first: int = 0, prompt: bool = False):
@@ -502,9 +614,26 @@ def attention_launch(shape: Shape) -> dict:
 
 def block8_plan(shape: Shape) -> dict:
     """ygg_debug_block8_plan: the launch plan of tree_attention_block8 for this shape (host only)."""
+    return _block_plan(shape, "ygg_debug_block8_plan")
+
+
+def block4_plan(shape: Shape) -> dict:
+    """ygg_debug_block4_plan: the launch plan of tree_attention_block4 for this shape (host only)."""
+    return _block_plan(shape, "ygg_debug_block4_plan")
+
+
+def prompt_plan(shape: Shape) -> dict:
+    """ygg_debug_prompt_plan: the launch plan of prompt_attention for this shape (host only)."""
+    cs = shape.c()
+    out = (ctypes.c_int32 * 3)()
+    _check(load_library().ygg_debug_prompt_plan(ctypes.byref(cs), out), "ygg_debug_prompt_plan")
+    return dict(rows=out[0], splits=out[1], tiles=out[2])
+
+
+def _block_plan(shape: Shape, name: str) -> dict:
     cs = shape.c()
     out = (ctypes.c_int32 * 7)()
-    _check(load_library().ygg_debug_block8_plan(ctypes.byref(cs), out), "ygg_debug_block8_plan")
+    _check(getattr(load_library(), name)(ctypes.byref(cs), out), name)
     return dict(row_blocks=out[0], row_tiles=out[1], rem_blocks=out[2], runs=out[3], rem_runs=out[4], wide=bool(out[5]), merge_lanes=out[6])
 
 

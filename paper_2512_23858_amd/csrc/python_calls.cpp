@@ -13,6 +13,7 @@
 
 #include <algorithm>
 #include <initializer_list>
+#include <type_traits>
 
 #include "ygg.h"
 
@@ -105,6 +106,23 @@ struct Args {
         if ((B > 1 && N > 1 && t.stride(0) != N * stride) || ((B > 1 || N > 1) && stride < inner)) { ok = false; return nullptr; }
         return t.data_ptr();
     }
+    // A tensor [N, ..] of rows likewise
+    void* flat_rows(int i, at::ScalarType want, int64_t& stride) {
+        PyObject* o = a[i];
+        stride = 0;
+        if (o == Py_None) return nullptr;
+        if (!THPVariable_Check(o)) { ok = false; return nullptr; }
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.is_cuda() || t.dim() < 2 || t.scalar_type() != want) { ok = false; return nullptr; }
+        int64_t inner = 1;
+        for (int64_t d = t.dim() - 1; d >= 1; --d) {
+            if (t.size(d) > 1 && t.stride(d) != inner) { ok = false; return nullptr; }
+            inner *= t.size(d);
+        }
+        stride = t.size(0) > 1 ? t.stride(0) : inner;
+        if (stride < inner) { ok = false; return nullptr; }
+        return t.data_ptr();
+    }
     // A given tensor has `per` elements to a sequence (the kernels go by the shape, not by the tensors).  More sequences may follow,
     // and a single one may be longer: where several are, the next one would not begin where the kernels step to.
     void holds(int i, int64_t seqs, int64_t per) {
@@ -118,6 +136,12 @@ struct Args {
         if (!ok || a[i] == Py_None) return;
         const at::Tensor& t = THPVariable_Unpack(a[i]);
         ok = t.size(0) == B && t.size(1) == N && t.numel() == B * N * inner;
+    }
+    // .. exactly so many rows, with `inner` elements to each
+    void flat_rows_are(int i, int64_t N, int64_t inner) {
+        if (!ok || a[i] == Py_None) return;
+        const at::Tensor& t = THPVariable_Unpack(a[i]);
+        ok = t.size(0) == N && t.numel() == N * inner;
     }
     // .. and exactly these dimensions behind a first one that is at least `layers`
     void layers_are(int i, int64_t layers, std::initializer_list<int64_t> behind) {
@@ -138,6 +162,8 @@ struct Args {
         return true;
     }
 };
+
+bool known_type(const ygg_shape& s) { return (s.kv_dtype >= YGG_F32 && s.kv_dtype <= YGG_FP8_BLOCK) || s.kv_dtype == YGG_FP4_BLOCK; }
 
 at::ScalarType kv_type(const ygg_shape& s) {
     return s.kv_dtype == YGG_F32 ? at::kFloat : s.kv_dtype == YGG_FP8_E4M3 ? at::kByte : at::kBFloat16;
@@ -165,7 +191,7 @@ PyObject* tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!arity(n, 12)) return nullptr;
     ygg_shape s{};
     Args t{a};
-    t.ok = read_shape(a[0], s) && s.kv_dtype >= 0 && s.kv_dtype <= 3;
+    t.ok = read_shape(a[0], s) && known_type(s);
     const at::ScalarType dt = kv_type(s);
     void *q = t.ptr(1, dt), *kc = t.ptr(2, dt), *vc = t.ptr(3, dt), *kt = t.ptr(5, dt), *vt = t.ptr(6, dt), *out = t.ptr(8, dt);
     int32_t *lens = t.ints(4), *parent = t.ints(7);
@@ -262,7 +288,7 @@ PyObject* accept_and_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!arity(n, 15)) return nullptr;
     ygg_shape s{};
     Args t{a};
-    t.ok = read_shape(a[0], s) && s.kv_dtype >= 0 && s.kv_dtype <= 3;
+    t.ok = read_shape(a[0], s) && known_type(s);
     const at::ScalarType dt = kv_type(s);
     int32_t layers = 0;
     t.number(1, layers);
@@ -289,26 +315,30 @@ bool cache_part(const at::Tensor& t, int64_t rank, int64_t layers, int64_t batch
 }
 
 // The six tensors of a block cache of so many layers (alone: and no more), from argument i on
-ygg_block8_cache block_cache(Args& t, int i, const ygg_shape& s, int64_t layers, bool alone) {
-    ygg_block8_cache c{};
+template <typename Cache>
+Cache block_cache(Args& t, int i, const ygg_shape& s, int64_t layers, bool alone) {
+    constexpr bool FOUR = std::is_same<Cache, ygg_block4_cache>::value;
+    Cache c{};
     c.k_codes = t.ptr(i, at::kByte); c.v_codes = t.ptr(i + 1, at::kByte);
-    c.k_scale = t.floats(i + 2); c.v_scale = t.floats(i + 3);
+    using Scale = decltype(c.k_scale);
+    c.k_scale = static_cast<Scale>(t.ptr(i + 2, FOUR ? at::kByte : at::kFloat)); c.v_scale = static_cast<Scale>(t.ptr(i + 3, FOUR ? at::kByte : at::kFloat));
     c.k_tail = t.ptr(i + 4, at::kBFloat16); c.v_tail = t.ptr(i + 5, at::kBFloat16);
-    const int64_t nblk = (s.kv_capacity + YGG_KV_BLOCK - 1) / YGG_KV_BLOCK, Hkv = s.n_kv_heads;
-    const int64_t per[3] = {Hkv * nblk * YGG_KV_BLOCK * s.head_dim, Hkv * nblk, Hkv * 2 * YGG_KV_BLOCK * s.head_dim}, rank[3] = {4, 3, 4};
+    const int64_t nblk = (s.kv_capacity + YGG_KV_BLOCK - 1) / YGG_KV_BLOCK, Hkv = s.n_kv_heads, Dh = s.head_dim;
+    const int64_t per[3] = {Hkv * nblk * YGG_KV_BLOCK * Dh / (FOUR ? 2 : 1), Hkv * nblk * (FOUR ? 2 * Dh : 1), Hkv * 2 * YGG_KV_BLOCK * Dh};
+    const int64_t rank[3] = {4, FOUR ? 4 : 3, 4};
     for (int k = 0; k < 6; ++k)
         if (t.ok && t.a[i + k] != Py_None)
             t.ok = cache_part(THPVariable_Unpack(t.a[i + k]), rank[k / 2], layers, s.batch, per[k / 2], alone);
     return c;
 }
 
-// (shape, q, k_codes, v_codes, k_scale, v_scale, k_tail, v_tail, seq_lens, k_tree, v_tree, parent_idx, out, lse, workspace)
-PyObject* tree_attention_block8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+template <typename Cache, typename Call>
+PyObject* tree_attention_block(PyObject* const* a, Py_ssize_t n, Call call) {
     if (!arity(n, 15)) return nullptr;
     ygg_shape s{};
     Args t{a};
     t.ok = read_shape(a[0], s);
-    const ygg_block8_cache c = block_cache(t, 2, s, 1, true);
+    const Cache c = block_cache<Cache>(t, 2, s, 1, true);
     void *q = t.ptr(1, at::kBFloat16), *kt = t.ptr(9, at::kBFloat16), *vt = t.ptr(10, at::kBFloat16), *out = t.ptr(12, at::kBFloat16);
     int32_t *lens = t.ints(8), *parent = t.ints(11);
     float* lse = t.floats(13);
@@ -318,11 +348,19 @@ PyObject* tree_attention_block8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     for (int i : {1, 12}) t.holds(i, B, N * s.n_q_heads * s.head_dim);
     for (int i : {9, 10}) t.holds(i, B, N * s.n_kv_heads * s.head_dim);
     t.holds(8, B, 1); t.holds(11, B, N); t.holds(13, B, N * s.n_q_heads);
-    return finish(t.ok, [&](void* st) { return ygg_tree_attention_block8(&s, q, &c, lens, kt, vt, parent, out, lse, ws, wn, st); });
+    return finish(t.ok, [&](void* st) { return call(&s, q, &c, lens, kt, vt, parent, out, lse, ws, wn, st); });
 }
 
-// (shape, n_layers, k_new, v_new, rows, n_new, seq_lens, k_codes, v_codes, k_scale, v_scale, k_tail, v_tail)
-PyObject* block8_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+// (shape, q, k_codes, v_codes, k_scale, v_scale, k_tail, v_tail, seq_lens, k_tree, v_tree, parent_idx, out, lse, workspace)
+PyObject* tree_attention_block8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return tree_attention_block<ygg_block8_cache>(a, n, ygg_tree_attention_block8);
+}
+PyObject* tree_attention_block4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return tree_attention_block<ygg_block4_cache>(a, n, ygg_tree_attention_block4);
+}
+
+template <typename Cache, typename Call>
+PyObject* block_append(PyObject* const* a, Py_ssize_t n, Call call) {
     if (!arity(n, 13)) return nullptr;
     ygg_shape s{};
     Args t{a};
@@ -331,12 +369,16 @@ PyObject* block8_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     t.number(1, layers);
     void *k = t.ptr(2, at::kBFloat16), *v = t.ptr(3, at::kBFloat16);
     int32_t *rows = t.ints(4), *n_new = t.ints(5), *lens = t.ints(6);
-    const ygg_block8_cache c = block_cache(t, 7, s, layers, false);
+    const Cache c = block_cache<Cache>(t, 7, s, layers, false);
     const int32_t n_rows = t.size(2, 2), most = rows ? t.size(4, 1) : n_rows;
     for (int i : {2, 3}) t.layers_are(i, layers, {s.batch, n_rows, s.n_kv_heads, s.head_dim});
     t.holds(4, s.batch, most); t.holds(5, s.batch, 1); t.holds(6, s.batch, 1);
-    return finish(t.ok, [&](void* st) { return ygg_block8_append(&s, layers, k, v, n_rows, rows, most, n_new, lens, &c, st); });
+    return finish(t.ok, [&](void* st) { return call(&s, layers, k, v, n_rows, rows, most, n_new, lens, &c, st); });
 }
+
+// (shape, n_layers, k_new, v_new, rows, n_new, seq_lens, k_codes, v_codes, k_scale, v_scale, k_tail, v_tail)
+PyObject* block8_append(PyObject*, PyObject* const* a, Py_ssize_t n) { return block_append<ygg_block8_cache>(a, n, ygg_block8_append); }
+PyObject* block4_append(PyObject*, PyObject* const* a, Py_ssize_t n) { return block_append<ygg_block4_cache>(a, n, ygg_block4_append); }
 
 // (shape, q, k, q_out, k_out, frequencies, seq_lens, parent_idx, positions, interleaved, scale)
 PyObject* tree_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -360,6 +402,62 @@ PyObject* tree_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return finish(t.ok && pairs <= 1024, [&](void* st) {
         return ygg_tree_rotary(&s, q, qs, k, ks, qo, ko, f, 2 * pairs, interleaved, (float)scale, lens, parent, positions, st);
     });
+}
+
+// (shape, q, k, q_out, k_out, q_weight, k_weight, frequencies, seq_lens, parent_idx, positions, interleaved, scale, eps)
+PyObject* tree_norm_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!arity(n, 14)) return nullptr;
+    ygg_shape s{};
+    Args t{a};
+    t.ok = read_shape(a[0], s);
+    const at::ScalarType dt = s.kv_dtype == YGG_F32 ? at::kFloat : at::kBFloat16;
+    int64_t qs, ks;
+    void *q = t.rows(1, dt, qs), *k = t.rows(2, dt, ks), *qo = t.ptr(3, dt), *ko = t.ptr(4, dt);
+    float *qw = t.floats(5), *kw = t.floats(6);
+    const double* f = t.typed<double>(7, at::kDouble);
+    const int32_t pairs = t.size(7, 0);
+    int32_t *lens = t.ints(8), *parent = t.ints(9), *positions = t.ints(10);
+    const int64_t B = s.batch, N = s.n_nodes, Dh = s.head_dim, q_row = s.n_q_heads * Dh, k_row = s.n_kv_heads * Dh;
+    t.rows_are(1, B, N, q_row); t.rows_are(2, B, N, k_row);
+    t.holds(3, B, N * q_row); t.holds(4, B, N * k_row); t.holds(10, B, N);
+    // weights of every head's own have two dimensions, in q's and k's alike
+    auto dims = [&](int i) -> int64_t { return t.ok && a[i] != Py_None ? THPVariable_Unpack(a[i]).dim() : 0; };
+    const bool per_head = dims(5) == 2 || dims(6) == 2;
+    for (int i : {5, 6})
+        if (t.ok && a[i] != Py_None) {
+            const at::Tensor& w = THPVariable_Unpack(a[i]);
+            t.ok = w.dim() == (per_head ? 2 : 1) && w.size(-1) == Dh && (!per_head || w.size(0) == (i == 5 ? s.n_q_heads : s.n_kv_heads));
+        }
+    if (!positions) { t.holds(8, B, 1); t.holds(9, B, N); }   // (else they are not read)
+    const bool interleaved = a[11] == Py_True;
+    const double scale = PyFloat_AsDouble(a[12]);
+    const double eps = PyErr_Occurred() ? -1.0 : PyFloat_AsDouble(a[13]);
+    if (PyErr_Occurred()) { PyErr_Clear(); t.ok = false; }
+    return finish(t.ok && pairs <= 1024, [&](void* st) {
+        return ygg_tree_norm_rotary(&s, q, qs, k, ks, qo, ko, qw, kw, per_head, (float)eps, f, 2 * pairs, interleaved, (float)scale, lens, parent,
+                                    positions, st);
+    });
+}
+
+// (shape, q, k, v, q_first, q_len, k_first, k_len, out, lse, workspace)
+PyObject* prompt_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!arity(n, 11)) return nullptr;
+    ygg_shape s{};
+    Args t{a};
+    t.ok = read_shape(a[0], s);
+    const at::ScalarType dt = s.kv_dtype == YGG_F32 ? at::kFloat : at::kBFloat16;
+    int64_t qs, ks, vs;
+    void *q = t.flat_rows(1, dt, qs), *k = t.flat_rows(2, dt, ks), *v = t.flat_rows(3, dt, vs), *out = t.ptr(8, dt);
+    int32_t *qf = t.ints(4), *ql = t.ints(5), *kf = t.ints(6), *kl = t.ints(7);
+    float* lse = t.floats(9);
+    size_t wn;
+    void* ws = t.scratch(10, wn);
+    const int64_t N = s.n_nodes, q_row = (int64_t)s.n_q_heads * s.head_dim, k_row = (int64_t)s.n_kv_heads * s.head_dim;
+    t.flat_rows_are(1, N, q_row);
+    for (int i : {2, 3}) t.flat_rows_are(i, s.kv_capacity, k_row);
+    t.holds(8, 1, N * q_row); t.holds(9, 1, N * s.n_q_heads);
+    for (int i : {4, 5, 6, 7}) t.holds(i, s.batch, 1);
+    return finish(t.ok, [&](void* st) { return ygg_prompt_attention(&s, q, qs, k, ks, v, vs, qf, ql, kf, kl, out, lse, ws, wn, st); });
 }
 
 // (shape, tokens, n_new, counts, rows, first, prompt)
@@ -426,7 +524,8 @@ PyMethodDef kMethods[] = {
     YGG_CALL(tree_attention), YGG_CALL(tree_attention_fp8kv), YGG_CALL(equal_growth_expand), YGG_CALL(equal_growth_expand_static),
     YGG_CALL(equal_growth_attach), YGG_CALL(prune_for_verification), YGG_CALL(accept_and_compact),
     YGG_CALL(tree_attention_block8), YGG_CALL(block8_append), YGG_CALL(tree_rotary), YGG_CALL(count_tokens),
-    YGG_CALL(constrain_logits), {nullptr, nullptr, 0, nullptr}};
+    YGG_CALL(constrain_logits), YGG_CALL(tree_norm_rotary), YGG_CALL(prompt_attention), YGG_CALL(block4_append),
+    YGG_CALL(tree_attention_block4), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_calls", "native argument marshalling of the launching calls", -1, kMethods,
                        nullptr, nullptr, nullptr, nullptr};

@@ -7,6 +7,7 @@
 // of q and k; the unrotated part of a head passes through the same units.  2 x 8191 tokens of 40 heads of 128, bf16: 68.2 us, 4.9 TB/s, a
 // copy's rate (past the caches it takes 81); 49 nodes for 16 requests of 72 heads 7.3 us; one token 2.2.
 #include "ygg_internal.h"
+#include "ygg_device.h"
 
 #include <hip/hip_bf16.h>
 
@@ -50,7 +51,9 @@ __device__ __forceinline__ void store8(T* p, const Vec8& v) {
     }
 }
 
-template <typename T, bool INTERLEAVED>
+// NORM: every head is scaled by its weights and the reciprocal of its root mean square first.  A head's units are neighbouring lanes, so
+// the sum of its squares meets in four or eight of them; a unit's weights come as its values do, and from L1 after the first token.
+template <typename T, bool INTERLEAVED, bool NORM>
 __global__ __launch_bounds__(kTokens * 64) void rotary_kernel(RotaryArgs a) {
     __shared__ int32_t parent_s[kMaxNodes];
     __shared__ float2 turn_s[kTokens][64];
@@ -97,6 +100,21 @@ __global__ __launch_bounds__(kTokens * 64) void rotary_kernel(RotaryArgs a) {
         const int first = !INTERLEAVED && turned ? 8 * k : 16 * k;
         const int second = !INTERLEAVED && turned ? 8 * k + pairs : 16 * k + 8;
         Vec8 x = load8(src + first), y = load8(src + second);
+        if constexpr (NORM) {
+            const float* w = (is_q ? a.q_weight : a.k_weight) + (a.weights_per_head ? (is_q ? head : head - a.Hq) * a.Dh : 0);
+            const Vec8 wx = load8(w + first), wy = load8(w + second);
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum = fmaf(x.x[e], x.x[e], fmaf(y.x[e], y.x[e], sum));
+            sum = group_reduce(sum, per_head, [](float p, float q) { return p + q; });   // (a head's lanes are all here or none)
+            const float mean = sum / (float)a.Dh + a.eps;
+            const float by = mean > 0.f ? 1.f / sqrtf(mean) : 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x.x[e] *= by * wx.x[e];
+                y.x[e] *= by * wy.x[e];
+            }
+        }
         if (turned) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -120,15 +138,23 @@ __global__ __launch_bounds__(kTokens * 64) void rotary_kernel(RotaryArgs a) {
 
 }  // namespace
 
-hipError_t launch_rotary(const RotaryArgs& a, bool f32, bool interleaved, hipStream_t st) {
+namespace {
+template <bool NORM>
+void launch_kind(const RotaryArgs& a, bool f32, bool interleaved, dim3 grid, hipStream_t st) {
+    if (f32 && interleaved) hipLaunchKernelGGL((rotary_kernel<float, true, NORM>), grid, dim3(kTokens * 64), 0, st, a);
+    else if (f32) hipLaunchKernelGGL((rotary_kernel<float, false, NORM>), grid, dim3(kTokens * 64), 0, st, a);
+    else if (interleaved) hipLaunchKernelGGL((rotary_kernel<uint16_t, true, NORM>), grid, dim3(kTokens * 64), 0, st, a);
+    else hipLaunchKernelGGL((rotary_kernel<uint16_t, false, NORM>), grid, dim3(kTokens * 64), 0, st, a);
+}
+}  // namespace
+
+hipError_t launch_rotary(const RotaryArgs& a, bool f32, bool interleaved, bool norm, hipStream_t st) {
     const int64_t tokens = (int64_t)a.B * a.N;
     const int64_t steps = (a.units + 63) / 64;   // of a wavefront that takes all heads of its token
     const int64_t split = std::clamp((int64_t)2048 / tokens, (int64_t)1, steps);
     const dim3 grid((unsigned)((a.N + kTokens - 1) / kTokens), (unsigned)a.B, (unsigned)split);
-    if (f32 && interleaved) hipLaunchKernelGGL((rotary_kernel<float, true>), grid, dim3(kTokens * 64), 0, st, a);
-    else if (f32) hipLaunchKernelGGL((rotary_kernel<float, false>), grid, dim3(kTokens * 64), 0, st, a);
-    else if (interleaved) hipLaunchKernelGGL((rotary_kernel<uint16_t, true>), grid, dim3(kTokens * 64), 0, st, a);
-    else hipLaunchKernelGGL((rotary_kernel<uint16_t, false>), grid, dim3(kTokens * 64), 0, st, a);
+    if (norm) launch_kind<true>(a, f32, interleaved, grid, st);
+    else launch_kind<false>(a, f32, interleaved, grid, st);
     return hipGetLastError();
 }
 

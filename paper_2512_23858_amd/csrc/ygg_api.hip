@@ -6,6 +6,7 @@
 #include <atomic>
 #include <cmath>
 #include <mutex>
+#include <type_traits>
 
 namespace ygg {
 namespace {
@@ -58,19 +59,34 @@ int32_t check_shape(const ygg_shape* s, bool need_kv, bool need_vocab) {
     return YGG_OK;
 }
 
-// Shapes of the calls on the 8-bit block cache.
-int32_t check_block8(const ygg_shape* s) {
+// Shapes of the calls on a block cache: dtype YGG_FP8_BLOCK or YGG_FP4_BLOCK.
+int32_t check_block(const ygg_shape* s, int32_t dtype) {
     if (int32_t rc = check_shape(s, false, false)) return rc;
-    if (s->kv_dtype != YGG_FP8_BLOCK || (s->head_dim != 64 && s->head_dim != 128)) return YGG_ERR_UNSUPPORTED;
+    if (s->kv_dtype != dtype || (s->head_dim != 64 && s->head_dim != 128)) return YGG_ERR_UNSUPPORTED;
     if (!(s->softmax_scale > 0.f) || !std::isfinite(s->softmax_scale)) return YGG_ERR_SHAPE;
     return YGG_OK;
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-int32_t check_cache(const ygg_block8_cache* c) {
+template <typename Cache>
+int32_t check_cache(const Cache* c) {
     if (!c || !c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale || !c->k_tail || !c->v_tail) return YGG_ERR_NULL;
     if (!aligned16(c->k_codes) || !aligned16(c->v_codes) || !aligned16(c->k_tail) || !aligned16(c->v_tail)) return YGG_ERR_UNSUPPORTED;
+    if (std::is_same<Cache, ygg_block4_cache>::value && (!aligned16(c->k_scale) || !aligned16(c->v_scale))) return YGG_ERR_UNSUPPORTED;
+    return YGG_OK;
+}
+
+// Shapes of ygg_prompt_attention: n_nodes rows of q, kv_capacity rows of k and v.
+int32_t check_prompt(const ygg_shape* s) {
+    if (!s) return YGG_ERR_NULL;
+    if (s->batch < 1 || s->batch > 65535 || s->n_q_heads < 1 || s->n_kv_heads < 1 || s->n_q_heads % s->n_kv_heads != 0 || s->n_nodes < 1 ||
+        s->max_seq_len < 0 || s->kv_capacity < 1 || s->kv_capacity < s->max_seq_len) return YGG_ERR_SHAPE;
+    if ((s->kv_dtype != YGG_F32 && s->kv_dtype != YGG_BF16) || (s->head_dim != 64 && s->head_dim != 128)) return YGG_ERR_UNSUPPORTED;
+    if (!(s->softmax_scale > 0.f) || !std::isfinite(s->softmax_scale)) return YGG_ERR_SHAPE;
+    // rows of a sequence and of the batch are counted with 31 bits
+    if (s->n_nodes > (1 << 25) || s->kv_capacity > 0x7fffffffLL || s->max_seq_len > (1 << 30) || (int64_t)s->n_nodes * s->n_q_heads > 0x7fffffffLL - 65536)
+        return YGG_ERR_UNSUPPORTED;
     return YGG_OK;
 }
 
@@ -273,8 +289,9 @@ static size_t attention_scratch_bytes(const ygg_shape& s) {
 }
 
 // Workgroup shapes and runs of the attention over the block cache.
-Block8Plan plan_block8(const ygg_shape& s) {
-    Block8Plan p{};
+BlockPlan plan_block(const ygg_shape& s, int bits) {
+    (void)bits;
+    BlockPlan p{};
     const int64_t R = (int64_t)s.n_nodes * (s.n_q_heads / s.n_kv_heads), row_blocks = (R + 31) / 32;
     // As many row blocks to a stream of keys as registers hold: for the 1284 rows of 321 nodes behind 32768 tokens eight take 165 us and
     // four 171.
@@ -342,8 +359,37 @@ Block8Plan plan_block8(const ygg_shape& s) {
 }
 
 // Workspace for this shape and every smaller max_seq_len: the most runs that any of them takes.
-static size_t block8_scratch_bytes(const ygg_shape& s, const Block8Plan& p) {
+static size_t block_scratch_bytes(const ygg_shape& s, const BlockPlan& p) {
     return part_o_bytes(s, true, p.most_runs) + part_rec_bytes(s, p.most_runs) + p.seq_splits_bytes;
+}
+
+// Workgroups and key splits of the attention of prompts.
+PromptPlan plan_prompt(const ygg_shape& s) {
+    PromptPlan p{};
+    const int64_t G = s.n_q_heads / s.n_kv_heads, rows = s.n_nodes * G, Hkv = s.n_kv_heads;
+    const bool f32 = s.kv_dtype == YGG_F32;
+    p.waves = f32 || rows / 256 * Hkv < 128 || rows / s.batch <= 128 ? 4 : 8;
+    const int64_t tile = 32 * p.waves;
+    const int64_t ranks = std::min(rows / tile + s.batch, rows);   // sum of ceil(rows_b / tile) over sequences that share no rows
+    p.ranks = (int32_t)ranks;
+    p.most_tiles = (int32_t)((rows + tile - 1) / tile);
+    const int64_t groups = std::max((rows + tile - 1) / tile, std::min((int64_t)s.batch, ranks)) * Hkv;
+    const int64_t tiles = (s.max_seq_len + kKeyTile - 1) / kKeyTile;
+    p.splits = f32 ? 1 : (int32_t)std::clamp(std::min(256 / groups, tiles / 4), (int64_t)1, (int64_t)32);
+    const int64_t merge = 256 / (s.head_dim / 8);
+    p.merge_ranks = (int32_t)std::min(rows / merge + s.batch, rows);
+    p.merge_most_tiles = (int32_t)((rows + merge - 1) / merge);
+    if (p.splits > 1) {
+        p.part_o_bytes = align256((size_t)p.splits * s.n_nodes * s.n_q_heads * s.head_dim * 2);
+        p.part_rec_bytes = align256((size_t)p.splits * s.n_nodes * s.n_q_heads * sizeof(float3));
+    }
+    return p;
+}
+
+// Workspace for this shape and every smaller max_seq_len: the splits do not fall with it.
+static size_t prompt_scratch_bytes(const ygg_shape& s) {
+    const PromptPlan p = plan_prompt(s);
+    return p.part_o_bytes + p.part_rec_bytes;
 }
 
 // Raises the shared-memory limits of the current device's kernels once; later calls cost one atomic load.
@@ -353,7 +399,8 @@ int32_t ensure_device_ready() {
     if (g_device_ready[dev].load(std::memory_order_acquire)) return YGG_OK;
     std::lock_guard<std::mutex> lock(g_init_mutex);
     if (g_device_ready[dev].load(std::memory_order_relaxed)) return YGG_OK;
-    if (raise_limits_attn_mfma() != hipSuccess || raise_limits_expand() != hipSuccess || raise_limits_attn_block8() != hipSuccess)
+    if (raise_limits_attn_mfma() != hipSuccess || raise_limits_expand() != hipSuccess || raise_limits_attn_block8() != hipSuccess ||
+        raise_limits_attn_block4() != hipSuccess || raise_limits_attn_prompt() != hipSuccess)
         return YGG_ERR_LAUNCH;
     void* sp = nullptr;
     if (hipGetSymbolAddress(&sp, HIP_SYMBOL(scratch)) != hipSuccess || !sp) return YGG_ERR_LAUNCH;
@@ -365,6 +412,98 @@ int32_t ensure_device_ready() {
 }  // namespace ygg
 
 using namespace ygg;
+
+template <typename Cache>
+static int32_t attention_block_impl(const ygg_shape* s, int bits, const void* q, const Cache* cache, const int32_t* seq_lens,
+                                  const void* k_tree, const void* v_tree, const int32_t* parent_idx, void* out, float* lse,
+                                  void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (int32_t rc = check_block(s, bits == 8 ? YGG_FP8_BLOCK : YGG_FP4_BLOCK)) return rc;
+    if (int32_t rc = check_cache(cache)) return rc;
+    if (!q || !seq_lens || !k_tree || !v_tree || !parent_idx || !out) return YGG_ERR_NULL;
+    if (!aligned16(q) || !aligned16(k_tree) || !aligned16(v_tree) || !aligned16(out)) return YGG_ERR_UNSUPPORTED;
+    const int64_t rows = (int64_t)s->batch * s->n_nodes * s->n_q_heads;
+    const BlockPlan p = plan_block(*s, bits);
+    // the kernels count query rows and a batch's blocks with 31 bits, and a launch's threads with 32
+    const int64_t streams = (p.runs ? (int64_t)p.runs + p.rem_runs : (int64_t)s->batch) * s->n_kv_heads + 8;
+    if (rows > 0x7fffffffLL || streams * (p.row_tiles + 1) > (1 << 22) || (int64_t)s->n_nodes * s->n_q_heads > (1 << 25) ||
+        (int64_t)s->batch * (s->max_seq_len / YGG_KV_BLOCK + p.lead + p.own) > 0x3fffffffLL) return YGG_ERR_UNSUPPORTED;
+    if (int32_t rc = check_workspace(workspace, workspace_bytes, block_scratch_bytes(*s, p))) return rc;
+    if (int32_t rc = ensure_device_ready()) return rc;
+
+    BlockArgs a{};
+    a.q = q; a.k_codes = cache->k_codes; a.v_codes = cache->v_codes; a.k_scale = cache->k_scale; a.v_scale = cache->v_scale;
+    a.k_tail = cache->k_tail; a.v_tail = cache->v_tail; a.k_tree = k_tree; a.v_tree = v_tree;
+    a.seq_lens = seq_lens; a.parent_idx = parent_idx;
+    a.part_o = workspace;
+    a.part_rec = reinterpret_cast<float3*>(static_cast<char*>(workspace) + p.part_o_bytes);
+    a.seq_splits = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + p.part_o_bytes + p.part_rec_bytes);
+    a.nblk = (s->kv_capacity + YGG_KV_BLOCK - 1) / YGG_KV_BLOCK;
+    a.rows_total = rows;
+    a.B = s->batch; a.N = s->n_nodes; a.Hq = s->n_q_heads; a.Hkv = s->n_kv_heads; a.G = a.Hq / a.Hkv; a.R = a.N * a.G;
+    a.out = out; a.lse = lse;
+    a.row_tiles = p.row_tiles; a.runs = p.runs; a.rem_runs = p.rem_runs; a.lead = p.lead; a.own = p.own;
+    a.main_rows = p.row_tiles * p.row_blocks * 32; a.max_seq_len = s->max_seq_len; a.scale = s->softmax_scale;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const hipError_t e = bits == 8 ? launch_attn_block8(a, p, s->head_dim, st) : launch_attn_block4(a, p, s->head_dim, st);
+    return e == hipSuccess ? YGG_OK : YGG_ERR_LAUNCH;
+}
+
+template <typename Cache>
+static int32_t block_append_impl(const ygg_shape* s, int bits, int32_t n_layers, const void* k_new, const void* v_new, int32_t n_rows,
+                          const int32_t* rows, int32_t max_new, const int32_t* n_new, const int32_t* seq_lens,
+                          const Cache* cache, void* hip_stream) {
+    if (int32_t rc = check_block(s, bits == 8 ? YGG_FP8_BLOCK : YGG_FP4_BLOCK)) return rc;
+    if (int32_t rc = check_cache(cache)) return rc;
+    if (!k_new || !v_new || !n_new || !seq_lens) return YGG_ERR_NULL;
+    if (n_layers < 1 || n_layers > 65535 || n_rows < 1 || max_new < 1 || (!rows && max_new > n_rows)) return YGG_ERR_SHAPE;
+    if (!aligned16(k_new) || !aligned16(v_new)) return YGG_ERR_UNSUPPORTED;
+    AppendArgs a{};
+    a.k_new = k_new; a.v_new = v_new; a.rows = rows; a.n_new = n_new; a.seq_lens = seq_lens;
+    a.k_codes = cache->k_codes; a.v_codes = cache->v_codes; a.k_scale = cache->k_scale; a.v_scale = cache->v_scale;
+    a.k_tail = cache->k_tail; a.v_tail = cache->v_tail;
+    a.nblk = (s->kv_capacity + YGG_KV_BLOCK - 1) / YGG_KV_BLOCK; a.cap = s->kv_capacity;
+    a.n_layers = n_layers; a.B = s->batch; a.Hkv = s->n_kv_heads; a.n_rows = n_rows; a.max_new = max_new;
+    a.blocks = (int32_t)(((int64_t)max_new + YGG_KV_BLOCK - 1) / YGG_KV_BLOCK);
+    if ((int64_t)n_layers * a.B * a.Hkv > (1 << 23) / a.blocks) return YGG_ERR_UNSUPPORTED;   // (the launch grid)
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const hipError_t e = bits == 8 ? launch_block8_append(a, s->head_dim, st) : launch_block4_append(a, s->head_dim, st);
+    return e == hipSuccess ? YGG_OK : YGG_ERR_LAUNCH;
+}
+
+static int32_t rotary_impl(const ygg_shape* s, const void* q, int64_t q_stride, const void* k, int64_t k_stride, void* q_out, void* k_out,
+                        const double* frequencies, int32_t rotary_dim, int32_t interleaved, float scale, const int32_t* seq_lens,
+                        const int32_t* parent_idx, const int32_t* positions, void* hip_stream, bool norm = false,
+                           const float* q_weight = nullptr, const float* k_weight = nullptr, bool per_head = false, float eps = 0.f) {
+    if (!s) return YGG_ERR_NULL;
+    if (!common_shape_ok(*s)) return YGG_ERR_SHAPE;
+    if (!positions && s->n_nodes > kMaxNodes) return YGG_ERR_UNSUPPORTED;
+    if (((s->kv_dtype < YGG_F32 || s->kv_dtype > YGG_FP8_BLOCK) && s->kv_dtype != YGG_FP4_BLOCK) || (s->head_dim != 64 && s->head_dim != 128)) return YGG_ERR_UNSUPPORTED;
+    if ((!q && !k) || (q && !q_out) || (k && !k_out) || !frequencies || (!positions && (!seq_lens || !parent_idx)) ||
+        (norm && ((q && !q_weight) || (k && !k_weight)))) return YGG_ERR_NULL;
+    if (rotary_dim < 16 || rotary_dim > s->head_dim || !std::isfinite(scale) || !(eps >= 0.f) || !std::isfinite(eps)) return YGG_ERR_SHAPE;
+    if (rotary_dim % 16) return YGG_ERR_UNSUPPORTED;
+    const bool f32 = s->kv_dtype == YGG_F32;
+    const int64_t q_dense = (int64_t)s->n_q_heads * s->head_dim, k_dense = (int64_t)s->n_kv_heads * s->head_dim;
+    const int64_t per16 = f32 ? 4 : 8;   // elements of 16 bytes
+    if (!q_stride) q_stride = q_dense;
+    if (!k_stride) k_stride = k_dense;
+    if ((q && (q_stride < q_dense || (q == q_out && q_stride != q_dense))) ||
+        (k && (k_stride < k_dense || (k == k_out && k_stride != k_dense)))) return YGG_ERR_SHAPE;
+    if ((q && (q_stride % per16 || !aligned16(q) || !aligned16(q_out))) || (k && (k_stride % per16 || !aligned16(k) || !aligned16(k_out))))
+        return YGG_ERR_UNSUPPORTED;
+    if (norm && ((q && !aligned16(q_weight)) || (k && !aligned16(k_weight)))) return YGG_ERR_UNSUPPORTED;
+    RotaryArgs a{};
+    a.q = q; a.k = k; a.q_out = q_out; a.k_out = k_out; a.frequencies = frequencies;
+    a.seq_lens = seq_lens; a.parent_idx = parent_idx; a.positions = positions;
+    a.q_stride = q_stride; a.k_stride = k_stride;
+    a.B = s->batch; a.N = s->n_nodes; a.Hq = q ? s->n_q_heads : 0; a.Hkv = k ? s->n_kv_heads : 0; a.Dh = s->head_dim;
+    const int64_t units = ((int64_t)a.Hq + a.Hkv) * (a.Dh / 16);
+    if (units > (1 << 22) || s->n_nodes > (1 << 25)) return YGG_ERR_UNSUPPORTED;   // (the launch grid)
+    a.units = (int32_t)units;
+    a.rotary_dim = rotary_dim; a.max_seq_len = s->max_seq_len; a.scale = scale;
+    a.q_weight = q_weight; a.k_weight = k_weight; a.weights_per_head = per_head; a.eps = eps;
+    return launch_rotary(a, f32, interleaved != 0, norm, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? YGG_OK : YGG_ERR_LAUNCH;
+}
 
 extern "C" {
 
@@ -394,12 +533,23 @@ int32_t ygg_debug_attention_launch(const ygg_shape* s, int32_t* launch) {
     return YGG_OK;
 }
 
-int32_t ygg_debug_block8_plan(const ygg_shape* s, int32_t* plan) {
-    if (int32_t rc = check_block8(s)) return rc;
+static int32_t block_plan_impl(const ygg_shape* s, int bits, int32_t* plan) {
+    if (int32_t rc = check_block(s, bits == 8 ? YGG_FP8_BLOCK : YGG_FP4_BLOCK)) return rc;
     if (!plan) return YGG_ERR_NULL;
-    const Block8Plan p = plan_block8(*s);
+    const BlockPlan p = plan_block(*s, bits);
     plan[0] = p.row_blocks; plan[1] = p.row_tiles; plan[2] = p.rem_blocks; plan[3] = p.runs; plan[4] = p.rem_runs;
     plan[5] = p.wide; plan[6] = p.merge_lanes;
+    return YGG_OK;
+}
+
+int32_t ygg_debug_block8_plan(const ygg_shape* s, int32_t* plan) { return block_plan_impl(s, 8, plan); }
+int32_t ygg_debug_block4_plan(const ygg_shape* s, int32_t* plan) { return block_plan_impl(s, 4, plan); }
+
+int32_t ygg_debug_prompt_plan(const ygg_shape* s, int32_t* plan) {
+    if (int32_t rc = check_prompt(s)) return rc;
+    if (!plan) return YGG_ERR_NULL;
+    const PromptPlan p = plan_prompt(*s);
+    plan[0] = 32 * p.waves; plan[1] = p.splits; plan[2] = p.ranks;
     return YGG_OK;
 }
 
@@ -433,8 +583,16 @@ size_t ygg_workspace_bytes(const ygg_shape* s, int32_t op, int32_t n_layers) {
             return accept_scratch_bytes(*s);
         }
         case YGG_OP_ATTENTION_BLOCK8: {
-            if (check_block8(s) != YGG_OK) return 0;
-            return block8_scratch_bytes(*s, plan_block8(*s));
+            if (check_block(s, YGG_FP8_BLOCK) != YGG_OK) return 0;
+            return block_scratch_bytes(*s, plan_block(*s, 8));
+        }
+        case YGG_OP_ATTENTION_BLOCK4: {
+            if (check_block(s, YGG_FP4_BLOCK) != YGG_OK) return 0;
+            return block_scratch_bytes(*s, plan_block(*s, 4));
+        }
+        case YGG_OP_PROMPT_ATTENTION: {
+            if (check_prompt(s) != YGG_OK) return 0;
+            return prompt_scratch_bytes(*s);
         }
         case YGG_OP_CONSTRAIN: {
             if (check_shape(s, false, true) != YGG_OK) return 0;
@@ -653,84 +811,68 @@ int32_t ygg_accept_and_compact(const ygg_shape* s, int32_t n_layers, const float
 int32_t ygg_tree_attention_block8(const ygg_shape* s, const void* q, const ygg_block8_cache* cache, const int32_t* seq_lens,
                                   const void* k_tree, const void* v_tree, const int32_t* parent_idx, void* out, float* lse,
                                   void* workspace, size_t workspace_bytes, void* hip_stream) {
-    if (int32_t rc = check_block8(s)) return rc;
-    if (int32_t rc = check_cache(cache)) return rc;
-    if (!q || !seq_lens || !k_tree || !v_tree || !parent_idx || !out) return YGG_ERR_NULL;
-    if (!aligned16(q) || !aligned16(k_tree) || !aligned16(v_tree) || !aligned16(out)) return YGG_ERR_UNSUPPORTED;
-    const int64_t rows = (int64_t)s->batch * s->n_nodes * s->n_q_heads;
-    const Block8Plan p = plan_block8(*s);
-    // the kernels count query rows and a batch's blocks with 31 bits, and a launch's threads with 32
-    const int64_t streams = (p.runs ? (int64_t)p.runs + p.rem_runs : (int64_t)s->batch) * s->n_kv_heads + 8;
-    if (rows > 0x7fffffffLL || streams * (p.row_tiles + 1) > (1 << 22) || (int64_t)s->n_nodes * s->n_q_heads > (1 << 25) ||
-        (int64_t)s->batch * (s->max_seq_len / YGG_KV_BLOCK + p.lead + p.own) > 0x3fffffffLL) return YGG_ERR_UNSUPPORTED;
-    if (int32_t rc = check_workspace(workspace, workspace_bytes, block8_scratch_bytes(*s, p))) return rc;
-    if (int32_t rc = ensure_device_ready()) return rc;
+    return attention_block_impl(s, 8, q, cache, seq_lens, k_tree, v_tree, parent_idx, out, lse, workspace, workspace_bytes, hip_stream);
+}
 
-    Block8Args a{};
-    a.q = q; a.k_codes = cache->k_codes; a.v_codes = cache->v_codes; a.k_scale = cache->k_scale; a.v_scale = cache->v_scale;
-    a.k_tail = cache->k_tail; a.v_tail = cache->v_tail; a.k_tree = k_tree; a.v_tree = v_tree;
-    a.seq_lens = seq_lens; a.parent_idx = parent_idx;
-    a.part_o = workspace;
-    a.part_rec = reinterpret_cast<float3*>(static_cast<char*>(workspace) + p.part_o_bytes);
-    a.seq_splits = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + p.part_o_bytes + p.part_rec_bytes);
-    a.nblk = (s->kv_capacity + YGG_KV_BLOCK - 1) / YGG_KV_BLOCK;
-    a.rows_total = rows;
-    a.B = s->batch; a.N = s->n_nodes; a.Hq = s->n_q_heads; a.Hkv = s->n_kv_heads; a.G = a.Hq / a.Hkv; a.R = a.N * a.G;
-    a.out = out; a.lse = lse;
-    a.row_tiles = p.row_tiles; a.runs = p.runs; a.rem_runs = p.rem_runs; a.lead = p.lead; a.own = p.own;
-    a.main_rows = p.row_tiles * p.row_blocks * 32; a.max_seq_len = s->max_seq_len; a.scale = s->softmax_scale;
-    hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    return launch_attn_block8(a, p, s->head_dim, st) == hipSuccess ? YGG_OK : YGG_ERR_LAUNCH;
+int32_t ygg_tree_attention_block4(const ygg_shape* s, const void* q, const ygg_block4_cache* cache, const int32_t* seq_lens,
+                                  const void* k_tree, const void* v_tree, const int32_t* parent_idx, void* out, float* lse,
+                                  void* workspace, size_t workspace_bytes, void* hip_stream) {
+    return attention_block_impl(s, 4, q, cache, seq_lens, k_tree, v_tree, parent_idx, out, lse, workspace, workspace_bytes, hip_stream);
 }
 
 int32_t ygg_block8_append(const ygg_shape* s, int32_t n_layers, const void* k_new, const void* v_new, int32_t n_rows,
                           const int32_t* rows, int32_t max_new, const int32_t* n_new, const int32_t* seq_lens,
                           const ygg_block8_cache* cache, void* hip_stream) {
-    if (int32_t rc = check_block8(s)) return rc;
-    if (int32_t rc = check_cache(cache)) return rc;
-    if (!k_new || !v_new || !n_new || !seq_lens) return YGG_ERR_NULL;
-    if (n_layers < 1 || n_layers > 65535 || n_rows < 1 || max_new < 1 || (!rows && max_new > n_rows)) return YGG_ERR_SHAPE;
-    if (!aligned16(k_new) || !aligned16(v_new)) return YGG_ERR_UNSUPPORTED;
-    AppendArgs a{};
-    a.k_new = k_new; a.v_new = v_new; a.rows = rows; a.n_new = n_new; a.seq_lens = seq_lens;
-    a.k_codes = cache->k_codes; a.v_codes = cache->v_codes; a.k_scale = cache->k_scale; a.v_scale = cache->v_scale;
-    a.k_tail = cache->k_tail; a.v_tail = cache->v_tail;
-    a.nblk = (s->kv_capacity + YGG_KV_BLOCK - 1) / YGG_KV_BLOCK; a.cap = s->kv_capacity;
-    a.n_layers = n_layers; a.B = s->batch; a.Hkv = s->n_kv_heads; a.n_rows = n_rows; a.max_new = max_new;
-    a.blocks = (int32_t)(((int64_t)max_new + YGG_KV_BLOCK - 1) / YGG_KV_BLOCK);
-    if ((int64_t)n_layers * a.B * a.Hkv > (1 << 23) / a.blocks) return YGG_ERR_UNSUPPORTED;   // (the launch grid)
-    return launch_block8_append(a, s->head_dim, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? YGG_OK : YGG_ERR_LAUNCH;
+    return block_append_impl(s, 8, n_layers, k_new, v_new, n_rows, rows, max_new, n_new, seq_lens, cache, hip_stream);
+}
+
+int32_t ygg_block4_append(const ygg_shape* s, int32_t n_layers, const void* k_new, const void* v_new, int32_t n_rows,
+                          const int32_t* rows, int32_t max_new, const int32_t* n_new, const int32_t* seq_lens,
+                          const ygg_block4_cache* cache, void* hip_stream) {
+    return block_append_impl(s, 4, n_layers, k_new, v_new, n_rows, rows, max_new, n_new, seq_lens, cache, hip_stream);
 }
 
 int32_t ygg_tree_rotary(const ygg_shape* s, const void* q, int64_t q_stride, const void* k, int64_t k_stride, void* q_out, void* k_out,
                         const double* frequencies, int32_t rotary_dim, int32_t interleaved, float scale, const int32_t* seq_lens,
                         const int32_t* parent_idx, const int32_t* positions, void* hip_stream) {
-    if (!s) return YGG_ERR_NULL;
-    if (!common_shape_ok(*s)) return YGG_ERR_SHAPE;
-    if (!positions && s->n_nodes > kMaxNodes) return YGG_ERR_UNSUPPORTED;
-    if (s->kv_dtype < YGG_F32 || s->kv_dtype > YGG_FP8_BLOCK || (s->head_dim != 64 && s->head_dim != 128)) return YGG_ERR_UNSUPPORTED;
-    if ((!q && !k) || (q && !q_out) || (k && !k_out) || !frequencies || (!positions && (!seq_lens || !parent_idx))) return YGG_ERR_NULL;
-    if (rotary_dim < 16 || rotary_dim > s->head_dim || !std::isfinite(scale)) return YGG_ERR_SHAPE;
-    if (rotary_dim % 16) return YGG_ERR_UNSUPPORTED;
+    return rotary_impl(s, q, q_stride, k, k_stride, q_out, k_out, frequencies, rotary_dim, interleaved, scale, seq_lens, parent_idx, positions,
+                       hip_stream);
+}
+
+int32_t ygg_tree_norm_rotary(const ygg_shape* s, const void* q, int64_t q_stride, const void* k, int64_t k_stride, void* q_out, void* k_out,
+                             const float* q_weight, const float* k_weight, int32_t weights_per_head, float eps, const double* frequencies,
+                             int32_t rotary_dim, int32_t interleaved, float scale, const int32_t* seq_lens, const int32_t* parent_idx,
+                             const int32_t* positions, void* hip_stream) {
+    return rotary_impl(s, q, q_stride, k, k_stride, q_out, k_out, frequencies, rotary_dim, interleaved, scale, seq_lens, parent_idx, positions,
+                       hip_stream, true, q_weight, k_weight, weights_per_head != 0, eps);
+}
+
+int32_t ygg_prompt_attention(const ygg_shape* s, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                             int64_t v_stride, const int32_t* q_first, const int32_t* q_len, const int32_t* k_first, const int32_t* k_len,
+                             void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (int32_t rc = check_prompt(s)) return rc;
+    if (!q || !k || !v || !q_first || !q_len || !k_first || !k_len || !out) return YGG_ERR_NULL;
     const bool f32 = s->kv_dtype == YGG_F32;
-    const int64_t q_dense = (int64_t)s->n_q_heads * s->head_dim, k_dense = (int64_t)s->n_kv_heads * s->head_dim;
-    const int64_t per16 = f32 ? 4 : 8;   // elements of 16 bytes
+    const int64_t q_dense = (int64_t)s->n_q_heads * s->head_dim, k_dense = (int64_t)s->n_kv_heads * s->head_dim, per16 = f32 ? 4 : 8;
     if (!q_stride) q_stride = q_dense;
     if (!k_stride) k_stride = k_dense;
-    if ((q && (q_stride < q_dense || (q == q_out && q_stride != q_dense))) ||
-        (k && (k_stride < k_dense || (k == k_out && k_stride != k_dense)))) return YGG_ERR_SHAPE;
-    if ((q && (q_stride % per16 || !aligned16(q) || !aligned16(q_out))) || (k && (k_stride % per16 || !aligned16(k) || !aligned16(k_out))))
+    if (!v_stride) v_stride = k_dense;
+    if (q_stride < q_dense || k_stride < k_dense || v_stride < k_dense) return YGG_ERR_SHAPE;
+    if (q_stride % per16 || k_stride % per16 || v_stride % per16 || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out))
         return YGG_ERR_UNSUPPORTED;
-    RotaryArgs a{};
-    a.q = q; a.k = k; a.q_out = q_out; a.k_out = k_out; a.frequencies = frequencies;
-    a.seq_lens = seq_lens; a.parent_idx = parent_idx; a.positions = positions;
-    a.q_stride = q_stride; a.k_stride = k_stride;
-    a.B = s->batch; a.N = s->n_nodes; a.Hq = q ? s->n_q_heads : 0; a.Hkv = k ? s->n_kv_heads : 0; a.Dh = s->head_dim;
-    const int64_t units = ((int64_t)a.Hq + a.Hkv) * (a.Dh / 16);
-    if (units > (1 << 22) || s->n_nodes > (1 << 25)) return YGG_ERR_UNSUPPORTED;   // (the launch grid)
-    a.units = (int32_t)units;
-    a.rotary_dim = rotary_dim; a.max_seq_len = s->max_seq_len; a.scale = scale;
-    return launch_rotary(a, f32, interleaved != 0, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? YGG_OK : YGG_ERR_LAUNCH;
+    if (k_stride > (1 << 24) || v_stride > (1 << 24)) return YGG_ERR_UNSUPPORTED;   // (32-bit offsets inside a tile of keys)
+    const PromptPlan p = plan_prompt(*s);
+    if ((int64_t)p.ranks * s->n_kv_heads * p.splits > (1 << 22) || (int64_t)p.merge_ranks * s->n_kv_heads > (1 << 23)) return YGG_ERR_UNSUPPORTED;   // (the launch grid)
+    if (int32_t rc = check_workspace(workspace, workspace_bytes, prompt_scratch_bytes(*s))) return rc;
+    if (int32_t rc = ensure_device_ready()) return rc;
+    PromptArgs a{};
+    a.q = q; a.k = k; a.v = v; a.q_first = q_first; a.q_len = q_len; a.k_first = k_first; a.k_len = k_len;
+    a.part_o = workspace;
+    a.part_rec = reinterpret_cast<float3*>(static_cast<char*>(workspace) + p.part_o_bytes);
+    a.out = out; a.lse = lse; a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride; a.k_rows = s->kv_capacity;
+    a.B = s->batch; a.Hq = s->n_q_heads; a.Hkv = s->n_kv_heads; a.G = a.Hq / a.Hkv; a.q_rows = s->n_nodes; a.max_keys = s->max_seq_len;
+    a.splits = p.splits; a.most_tiles = p.most_tiles; a.scale = s->softmax_scale;
+    return launch_attn_prompt(a, p, s->head_dim, f32, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? YGG_OK : YGG_ERR_LAUNCH;
 }
 
 int32_t ygg_count_tokens(const ygg_shape* s, const int32_t* tokens, int32_t n_tokens, const int32_t* rows, int32_t first, int32_t max_new,

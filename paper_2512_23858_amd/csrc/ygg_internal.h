@@ -156,8 +156,8 @@ AcceptPlan plan_accept(const ygg_shape& s);
 size_t accept_scratch_bytes(const ygg_shape& s);
 hipError_t launch_accept(const AcceptArgs& a, hipStream_t st);
 
-// ---- attention over the 8-bit block cache ----------------------------------------------------------
-struct Block8Plan {
+// ---- attention over the 8-bit and the 4-bit block cache --------------------------------------------
+struct BlockPlan {
     int32_t row_blocks;   // 32-row blocks to a workgroup: 1, 2, 4 or 8
     int32_t row_tiles;    // workgroups of that shape along the N*G query rows of one kv head
     int32_t rem_blocks;   // 2 or 4: the rows beyond them go to workgroups of that many row blocks; 0: there are none
@@ -168,12 +168,12 @@ struct Block8Plan {
     int32_t merge_lanes;  // lanes to a row of the merge of partials: a wavefront's or as many as hold the row once; 0: no sequence is cut
     size_t part_o_bytes, part_rec_bytes, seq_splits_bytes;
 };
-struct Block8Args {
+struct BlockArgs {
     const void* q;
     const void* k_codes;
     const void* v_codes;
-    const float* k_scale;
-    const float* v_scale;
+    const void* k_scale;   // fp32, or the 4-bit cache's bytes
+    const void* v_scale;
     const void* k_tail;
     const void* v_tail;
     const void* k_tree;
@@ -193,11 +193,42 @@ struct Block8Args {
     int32_t stat_at;               // bytes of shared memory in front of the rows' statistics
     float scale;
 };
-Block8Plan plan_block8(const ygg_shape& s);
-hipError_t launch_attn_block8(const Block8Args& a, const Block8Plan& p, int head_dim, hipStream_t st);
+BlockPlan plan_block(const ygg_shape& s, int bits);
+hipError_t launch_attn_block8(const BlockArgs& a, const BlockPlan& p, int head_dim, hipStream_t st);
 hipError_t raise_limits_attn_block8();
+hipError_t launch_attn_block4(const BlockArgs& a, const BlockPlan& p, int head_dim, hipStream_t st);
+hipError_t raise_limits_attn_block4();
 
-// ---- appending to the 8-bit block cache ------------------------------------------------------------
+// ---- attention of prompts ----------------------------------------------------------------------------
+struct PromptPlan {
+    int32_t waves;         // wavefronts of 32 rows to a workgroup: 8 or 4
+    int32_t splits;        // parts of a row tile's keys
+    int32_t ranks;         // row tiles that there can be
+    int32_t most_tiles;    // .. of one sequence
+    int32_t merge_ranks, merge_most_tiles;   // the same in the merge's units
+    size_t part_o_bytes, part_rec_bytes;
+};
+struct PromptArgs {
+    const void* q;
+    const void* k;
+    const void* v;
+    const int32_t* q_first;
+    const int32_t* q_len;
+    const int32_t* k_first;
+    const int32_t* k_len;
+    void* part_o;          // [splits][q_rows * Hq][Dh] fp16, relative to the row's largest magnitude
+    float3* part_rec;      // [splits][q_rows * Hq] {reference in base-2 units (-inf: no key), sum, that magnitude}
+    void* out;
+    float* lse;
+    int64_t q_stride, k_stride, v_stride, k_rows;
+    int32_t B, Hq, Hkv, G, q_rows, max_keys, splits, most_tiles;
+    float scale;
+};
+PromptPlan plan_prompt(const ygg_shape& s);
+hipError_t launch_attn_prompt(const PromptArgs& a, const PromptPlan& p, int head_dim, bool f32, hipStream_t st);
+hipError_t raise_limits_attn_prompt();
+
+// ---- appending to the block caches ------------------------------------------------------------
 struct AppendArgs {
     const void* k_new;
     const void* v_new;
@@ -206,8 +237,8 @@ struct AppendArgs {
     const int32_t* seq_lens;
     void* k_codes;
     void* v_codes;
-    float* k_scale;
-    float* v_scale;
+    void* k_scale;         // fp32, or the 4-bit cache's bytes
+    void* v_scale;
     void* k_tail;
     void* v_tail;
     int64_t nblk, cap;
@@ -215,6 +246,7 @@ struct AppendArgs {
     int32_t blocks;        // touched blocks that the new tokens can complete, at least 1
 };
 hipError_t launch_block8_append(const AppendArgs& a, int head_dim, hipStream_t st);
+hipError_t launch_block4_append(const AppendArgs& a, int head_dim, hipStream_t st);
 
 // ---- rotary positions --------------------------------------------------------------------------------
 struct RotaryArgs {
@@ -231,8 +263,12 @@ struct RotaryArgs {
     int32_t units;              // pieces of 16 elements of a token, (Hq + Hkv) * Dh / 16
     int32_t rotary_dim, max_seq_len;
     float scale;
+    const float* q_weight;      // norms: [Dh], or [heads][Dh]
+    const float* k_weight;
+    float eps;
+    int32_t weights_per_head;
 };
-hipError_t launch_rotary(const RotaryArgs& a, bool f32, bool interleaved, hipStream_t st);
+hipError_t launch_rotary(const RotaryArgs& a, bool f32, bool interleaved, bool norm, hipStream_t st);
 
 // ---- constraints on logits -----------------------------------------------------------------------------
 struct ConstrainArgs {
