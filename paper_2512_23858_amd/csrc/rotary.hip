@@ -97,8 +97,9 @@ __global__ __launch_bounds__(kTokens * 64) void rotary_kernel(RotaryArgs a) {
         T* dst = is_q ? static_cast<T*>(a.q_out) + (row * a.Hq + head) * a.Dh
                       : static_cast<T*>(a.k_out) + (row * a.Hkv + head - a.Hq) * a.Dh;
         const bool turned = k < rotated;
-        const int first = !INTERLEAVED && turned ? 8 * k : 16 * k;
-        const int second = !INTERLEAVED && turned ? 8 * k + pairs : 16 * k + 8;
+        // interleaved: pieces half a head apart, each turned or not by itself, so that neighbouring lanes' pieces are neighbours
+        const int first = INTERLEAVED || turned ? 8 * k : 16 * k;
+        const int second = INTERLEAVED ? 8 * k + a.Dh / 2 : turned ? 8 * k + pairs : 16 * k + 8;
         Vec8 x = load8(src + first), y = load8(src + second);
         if constexpr (NORM) {
             const float* w = (is_q ? a.q_weight : a.k_weight) + (a.weights_per_head ? (is_q ? head : head - a.Hq) * a.Dh : 0);
@@ -107,28 +108,34 @@ __global__ __launch_bounds__(kTokens * 64) void rotary_kernel(RotaryArgs a) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum = fmaf(x.x[e], x.x[e], fmaf(y.x[e], y.x[e], sum));
             sum = group_reduce(sum, per_head, [](float p, float q) { return p + q; });   // (a head's lanes are all here or none)
-            const float mean = sum / (float)a.Dh + a.eps;
-            const float by = mean > 0.f ? 1.f / sqrtf(mean) : 0.f;
+            const float mean = fmaf(sum, a.Dh == 128 ? 0x1p-7f : 0x1p-6f, a.eps);
+            const float by = mean > 0.f ? rsqrtf(mean) : 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 x.x[e] *= by * wx.x[e];
                 y.x[e] *= by * wy.x[e];
             }
         }
-        if (turned) {
+        if constexpr (INTERLEAVED) {
+            auto turn = [&](Vec8& v, int at) {
+                if (at >= a.rotary_dim) return;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 t = turn_s[wave][at / 2 + e];
+                    const float p = v.x[2 * e], q = v.x[2 * e + 1];
+                    v.x[2 * e] = p * t.x - q * t.y;
+                    v.x[2 * e + 1] = q * t.x + p * t.y;
+                }
+            };
+            turn(x, first);
+            turn(y, second);
+        } else if (turned) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float2 t = turn_s[wave][8 * k + e];
-                if constexpr (INTERLEAVED) {
-                    Vec8& v = e < 4 ? x : y;
-                    const float p = v.x[2 * (e % 4)], q = v.x[2 * (e % 4) + 1];
-                    v.x[2 * (e % 4)] = p * t.x - q * t.y;
-                    v.x[2 * (e % 4) + 1] = q * t.x + p * t.y;
-                } else {
-                    const float p = x.x[e], q = y.x[e];
-                    x.x[e] = p * t.x - q * t.y;
-                    y.x[e] = q * t.x + p * t.y;
-                }
+                const float p = x.x[e], q = y.x[e];
+                x.x[e] = p * t.x - q * t.y;
+                y.x[e] = q * t.x + p * t.y;
             }
         }
         store8(dst + first, x);
