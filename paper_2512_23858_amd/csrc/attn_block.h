@@ -33,15 +33,16 @@ struct Layout {
     static constexpr int SCALES = BITS == 4 ? 256 : 0;    // room for its scales
     static constexpr int SHARE = 2 * CODES + 2 * SCALES;  // [K codes, V codes, K scales, V scales]
     static constexpr int STAGE = KS * SHARE;              // [share]
-    static constexpr int NSTAGE = BITS == 4 ? 4 : 2;
+    static constexpr int NSTAGE = BITS == 4 && RB > 1 ? 4 : 2;
     static constexpr int HALF = kT * DH;                  // own keys: 32 rows of K (or V)
     static constexpr int OWN_CHUNKS = HALF / 1024;
     static constexpr int OWN_LOADS = 2 * OWN_CHUNKS / RB;
-    static constexpr int OWN_STAGE = KS * 2 * HALF;       // [share][K, V], two of them
+    static constexpr int OWN_STAGE = KS * 2 * HALF;       // [share][K, V]
+    static constexpr int OWN_STAGES = RB == 1 && KS >= 4 ? 1 : 2;   // one row block has three tiles of own keys at most: one step
     static constexpr int OROW = DH + 4;                   // floats of a row of O~ in LDS
     static constexpr int MERGE = NW * 32 * OROW * 4;      // in the tiles' place
     static constexpr int STAT = NW * 32 * 2 * 4;          // (reference, sum) of every wavefront's rows, behind everything else
-    static constexpr int TREE = std::max(NSTAGE * STAGE, 2 * OWN_STAGE);   // parents, then masks, behind the tiles
+    static constexpr int TREE = std::max(NSTAGE * STAGE, OWN_STAGES * OWN_STAGE);   // parents, then masks, behind the tiles
     static size_t smem(int nodes) {
         const int tree = TREE + nodes * 4 + RB * 32 * ((nodes + 31) / 32) * 4;
         return (size_t)(std::max(MERGE, tree) + 15) / 16 * 16 + STAT;
@@ -124,7 +125,7 @@ __device__ __forceinline__ void write_rows(unsigned char* smem, float* stat, Row
     const int n = lane & 31, half = lane >> 5;
     float* const o_s = reinterpret_cast<float*>(smem);
     const float l = both_halves_sum(x.l);
-    __syncthreads();   // the tiles are read
+    lds_barrier();   // the tiles are read  (a barrier of LDS alone: a full one would await the rows' way to memory)
 #pragma unroll
     for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
@@ -135,7 +136,7 @@ __device__ __forceinline__ void write_rows(unsigned char* smem, float* stat, Row
         stat[(wave * 32 + n) * 2] = x.any ? (float)x.ref : -INFINITY;
         stat[(wave * 32 + n) * 2 + 1] = l;
     }
-    __syncthreads();
+    lds_barrier();
     constexpr int LPR = DH / 8;   // lanes of a row
     for (int it = tid; it < RB * 32 * LPR; it += NW * 64) {
         const int r = it / LPR, col = it % LPR;
@@ -182,7 +183,7 @@ __device__ __forceinline__ void write_rows(unsigned char* smem, float* stat, Row
             if (col == 0) a.part_rec[at] = make_float3(m, sum, c);
         }
     }
-    __syncthreads();   // before the next segment's tiles
+    lds_barrier();   // before the next segment's tiles
 }
 
 // The open block's rows and the tree's keys under the ancestor mask, 32 to a tile: units 0 and 1 are the open block's, 2 + k the tree's
@@ -229,8 +230,9 @@ __device__ __forceinline__ void own_keys(unsigned char* smem, Rows<DH>& x, int b
             dma_load16_flat<false>((is_v ? vb : kb) + min(r, last) * row_b + 16 * at, to + (is_v ? Lay::HALF : 0) + chunk * 1024);
         }
     };
-    __syncthreads();   // the blocks' tiles are read
+    lds_barrier();   // the blocks' tiles are read
     fill(0);
+    if (steps > 1) fill(1);
     const int row = min(row0 + rb * 32 + n, a.R - 1);
     const int node = row / a.G, h = g * a.G + row % a.G;
     i32x4 q[NK];
@@ -240,7 +242,7 @@ __device__ __forceinline__ void own_keys(unsigned char* smem, Rows<DH>& x, int b
     for (int j = tid; j < seen_nodes; j += NW * 64) parent_s[j] = a.parent_idx[(int64_t)b * a.N + j];
     if (share == 0)
         for (int w = lane; w < 32 * words; w += 64) mask_s[w] = 0;
-    __syncthreads();
+    lds_barrier();
     if (share == 0 && half == 0)   // a lane per row; a parent that is no earlier node ends the walk
         for (int j = node;;) {
             mask_s[(j >> 5) * 32 + n] |= 1u << (j & 31);
@@ -254,9 +256,12 @@ __device__ __forceinline__ void own_keys(unsigned char* smem, Rows<DH>& x, int b
     const int v_lane = v_row * ROWB + 8 * (lane & 3), v_pair = (lane >> 4) & 1, v_xor = (v_row & (NDB - 1)) << 1;
     const float scale = a.scale * kLog2e;
     for (int step = 0; step < steps; ++step) {
-        dma_wait_keep<0>();
-        __syncthreads();
-        fill(step + 1);
+        if (step > 0 && step + 1 < steps) {
+            lds_barrier();      // the step before this has been read
+            fill(step + 1);
+        }
+        if (step + 1 < steps) dma_wait_keep<Lay::OWN_LOADS>(); else dma_wait_keep<0>();
+        lds_barrier();
         const int tile = step * KS + share;
         if (tile >= tiles || !active) continue;
         const bool in_tree = tile >= n_open;
@@ -381,10 +386,10 @@ __global__ __launch_bounds__(256) void block_merge_kernel(BlockArgs a) {
     if (row >= rows) return;   // (a row's lanes go together)
     const int col = threadIdx.x % LPR, grp = threadIdx.x % LANES / LPR;
     const int local = row / a.Hq * a.G + row % a.Hq % a.G;
-    const int splits = a.seq_splits[local < a.main_rows ? b : a.B + b];
-    if (splits == 0) return;   // final already
     const int64_t r = (int64_t)b * rows + row;
     const f16x8* const po = static_cast<const f16x8*>(a.part_o) + r * LPR + col;
+    const int splits = a.seq_splits[local < a.main_rows ? b : a.B + b];
+    if (splits == 0) return;   // final already
     float m = -INFINITY, l = 0.f, acc[8] = {};
     for (int s0 = grp; s0 < splits; s0 += GRP * AT_ONCE) {
         float3 rec[AT_ONCE];
@@ -471,7 +476,9 @@ hipError_t launch(BlockArgs a, int merge_lanes, hipStream_t st) {
 template <int BITS, int DH>
 hipError_t launch_for(const BlockArgs& a, const BlockPlan& p, hipStream_t st) {
     switch (p.row_blocks * 10 + p.rem_blocks) {
-        case 10: return p.wide ? launch<BITS, DH, 4, 1, 0>(a, p.merge_lanes, st) : launch<BITS, DH, 2, 1, 0>(a, p.merge_lanes, st);
+        case 10:
+            if constexpr (BITS == 4) return p.wide ? launch<BITS, DH, 8, 1, 0>(a, p.merge_lanes, st) : launch<BITS, DH, 4, 1, 0>(a, p.merge_lanes, st);
+            else return p.wide ? launch<BITS, DH, 4, 1, 0>(a, p.merge_lanes, st) : launch<BITS, DH, 2, 1, 0>(a, p.merge_lanes, st);
         case 20: return p.wide ? launch<BITS, DH, 8, 2, 0>(a, p.merge_lanes, st) : launch<BITS, DH, 4, 2, 0>(a, p.merge_lanes, st);
         case 40: return p.wide ? launch<BITS, DH, 8, 4, 0>(a, p.merge_lanes, st) : launch<BITS, DH, 4, 4, 0>(a, p.merge_lanes, st);
         case 80: return launch<BITS, DH, 8, 8, 0>(a, p.merge_lanes, st);
@@ -484,8 +491,8 @@ hipError_t launch_for(const BlockArgs& a, const BlockPlan& p, hipStream_t st) {
 template <int BITS, int DH>
 hipError_t raise_for() {
     hipError_t e = hipSuccess;
-    for (hipError_t x : {raise<BITS, DH, 2, 1, 0>(), raise<BITS, DH, 4, 2, 0>(), raise<BITS, DH, 4, 4, 0>(), raise<BITS, DH, 4, 1, 0>(), raise<BITS, DH, 8, 2, 0>(),
-                         raise<BITS, DH, 8, 4, 0>(), raise<BITS, DH, 8, 8, 0>(), raise<BITS, DH, 8, 8, 2>(), raise<BITS, DH, 8, 8, 4>()})
+    for (hipError_t x : {raise<BITS, DH, BITS == 4 ? 8 : 2, 1, 0>(), raise<BITS, DH, 4, 2, 0>(), raise<BITS, DH, 4, 4, 0>(), raise<BITS, DH, 4, 1, 0>(),
+                         raise<BITS, DH, 8, 2, 0>(), raise<BITS, DH, 8, 4, 0>(), raise<BITS, DH, 8, 8, 0>(), raise<BITS, DH, 8, 8, 2>(), raise<BITS, DH, 8, 8, 4>()})
         if (x != hipSuccess) e = x;
     return e;
 }
