@@ -335,7 +335,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void prompt_kernel(PromptArgs a) {
         int t = 0;
         if constexpr (PHASES) {
             if (late) step();
-            const int steady_end = (clean - base) / kKeys - 3;   // (clean may lie below base: then there is none)
+            const int steady_end = min((clean - base) / kKeys, ntiles) - 3;   // (clean may lie below base, or beyond this part of the keys)
             while (t < ntiles) {
                 body(t, t % NBUF, std::false_type{});
                 ++t;
@@ -414,17 +414,33 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptArgs a) {
     if (row >= R) return;
     const int query = row / a.G, head = g * a.G + row % a.G;
     const int64_t at = (int64_t)(q0 + query) * a.Hq + head, rows = (int64_t)a.q_rows * a.Hq;
-    float m = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_rec[s * rows + at].x);
-    float l = 0.f, acc[8] = {};
-    for (int s = 0; s < a.splits; ++s) {
-        const float3 rec = a.part_rec[s * rows + at];
-        if (rec.x == -INFINITY) continue;
-        const float w = __builtin_amdgcn_exp2f(rec.x - m);
-        l = fmaf(rec.y, w, l);
-        const f16x8 y = *reinterpret_cast<const f16x8*>(static_cast<const _Float16*>(a.part_o) + (s * rows + at) * DH + 8 * col);
+    constexpr int AT_ONCE = 8;   // partials requested together (one after the other, 31 of them took 28 us)
+    float m = -INFINITY, l = 0.f, acc[8] = {};
+    for (int s0 = 0; s0 < a.splits; s0 += AT_ONCE) {
+        float3 rec[AT_ONCE];
+        f16x8 raw[AT_ONCE];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] = fmaf((float)y[e], w * rec.z, acc[e]);
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const int64_t r = min(s0 + u, a.splits - 1) * rows + at;
+            rec[u] = a.part_rec[r];
+            raw[u] = *reinterpret_cast<const f16x8*>(static_cast<const _Float16*>(a.part_o) + r * DH + 8 * col);
+        }
+        float top = m;
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) top = fmaxf(top, rec[u].x);
+        const float fix = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        l *= fix;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] *= fix;
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {   // (a part without keys has written zeros)
+            const float w = s0 + u < a.splits && rec[u].x != -INFINITY ? __builtin_amdgcn_exp2f(rec[u].x - top) : 0.f;
+            l = fmaf(rec[u].y, w, l);
+            const float wc = w * rec[u].z;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] = fmaf((float)raw[u][e], wc, acc[e]);
+        }
+        m = top;
     }
     const float by = l > 0.f ? 1.f / l : 0.f;
     u32x4 y;

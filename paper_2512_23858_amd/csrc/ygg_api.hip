@@ -365,33 +365,65 @@ static size_t block_scratch_bytes(const ygg_shape& s, const BlockPlan& p) {
     return part_o_bytes(s, true, p.most_runs) + part_rec_bytes(s, p.most_runs) + p.seq_splits_bytes;
 }
 
-// Workgroups and key splits of the attention of prompts.
+static size_t prompt_part_o_bytes(const ygg_shape& s, int64_t splits) { return align256((size_t)splits * s.n_nodes * s.n_q_heads * s.head_dim * 2); }
+static size_t prompt_part_rec_bytes(const ygg_shape& s, int64_t splits) { return align256((size_t)splits * s.n_nodes * s.n_q_heads * sizeof(float3)); }
+
+// Workgroups and key splits of the attention of prompts: row tiles of 256 or of 128 rows, and where these leave compute units without work
+// their keys in parts.  The kind of least estimated time, from a start and a time per tile of 64 keys (us, fitted): 256 rows take as long per
+// tile as 128 at head_dim 128, where either has its compute unit to itself, but start later; at head_dim 64 three workgroups of 128 rows
+// share one.  us per call, 128 rows / 256: a prompt of 512 tokens with heads 32/8 of 128 18 / 21, of 2048 63 / 54, of 8192 718 / 462,
+// 64 of 60 tokens 37 / 29, 300 tokens behind 16000 138 / 87, 64 behind 8000 26 / 29; heads 12 of 64, eight of 90 to 2047 tokens 41.5 / 45.5,
+// 32/8 of 64, of 4096 tokens 107 / 93.  Without parts: 64 tokens behind 8000 185, 16 behind 30000 (heads 64/8) 680 (with: 26 and 40).
 PromptPlan plan_prompt(const ygg_shape& s) {
+    struct Kind { int32_t waves; float start, tile, shared; int64_t at_once; };   // shared: time per tile of a workgroup among several
+    static constexpr Kind kinds128[] = {{4, 10.f, 1.15f, 1.15f, 256}, {8, 14.f, 1.25f, 1.25f, 256}};
+    static constexpr Kind kinds64[] = {{4, 8.f, 0.95f, 0.72f, 768}, {8, 13.f, 1.15f, 1.15f, 256}};
     PromptPlan p{};
     const int64_t G = s.n_q_heads / s.n_kv_heads, rows = s.n_nodes * G, Hkv = s.n_kv_heads;
     const bool f32 = s.kv_dtype == YGG_F32;
-    p.waves = f32 || rows / 256 * Hkv < 128 || rows / s.batch <= 128 ? 4 : 8;
+    const int64_t each = (rows + s.batch - 1) / s.batch;   // rows of a sequence, if all are alike
+    const int64_t tiles = std::max((s.max_seq_len + kKeyTile - 1) / kKeyTile, 1);
+    // keys of a row tile on average: half of them in a prompt from its start on, nearly all of them in one's later chunk
+    const int64_t queries = (s.n_nodes + s.batch - 1) / s.batch;
+    const float mean = s.max_seq_len <= 2 * queries ? 0.5f * (float)(tiles + 1) : (float)tiles - 0.5f * (float)queries / kKeyTile;
+    float least = 0.f;
+    for (const Kind& k : s.head_dim == 128 ? kinds128 : kinds64) {
+        const int64_t tile = 32 * k.waves, groups = (each + tile - 1) / tile * std::min((int64_t)s.batch, rows) * Hkv;
+        const int64_t splits = f32 ? 1 : std::clamp(std::min(256 / groups, tiles / 4), (int64_t)1, (int64_t)32);
+        const float time = k.start * (float)((groups * splits + k.at_once - 1) / k.at_once) +
+                           std::max(k.tile * (float)((tiles + splits - 1) / splits), k.shared * mean * (float)groups / 256.f) +
+                           (splits > 1 ? 4.f + 0.1f * (float)splits : 0.f);
+        if (p.waves == 0 || (time < least && !f32)) {
+            least = time;
+            p.waves = k.waves;
+            p.splits = (int32_t)splits;
+        }
+    }
     const int64_t tile = 32 * p.waves;
-    const int64_t ranks = std::min(rows / tile + s.batch, rows);   // sum of ceil(rows_b / tile) over sequences that share no rows
-    p.ranks = (int32_t)ranks;
+    p.ranks = (int32_t)std::min(rows / tile + s.batch, rows);   // sum of ceil(rows_b / tile) over sequences that share no rows
     p.most_tiles = (int32_t)((rows + tile - 1) / tile);
-    const int64_t groups = std::max((rows + tile - 1) / tile, std::min((int64_t)s.batch, ranks)) * Hkv;
-    const int64_t tiles = (s.max_seq_len + kKeyTile - 1) / kKeyTile;
-    p.splits = f32 ? 1 : (int32_t)std::clamp(std::min(256 / groups, tiles / 4), (int64_t)1, (int64_t)32);
     const int64_t merge = 256 / (s.head_dim / 8);
     p.merge_ranks = (int32_t)std::min(rows / merge + s.batch, rows);
     p.merge_most_tiles = (int32_t)((rows + merge - 1) / merge);
     if (p.splits > 1) {
-        p.part_o_bytes = align256((size_t)p.splits * s.n_nodes * s.n_q_heads * s.head_dim * 2);
-        p.part_rec_bytes = align256((size_t)p.splits * s.n_nodes * s.n_q_heads * sizeof(float3));
+        p.part_o_bytes = prompt_part_o_bytes(s, p.splits);
+        p.part_rec_bytes = prompt_part_rec_bytes(s, p.splits);
     }
     return p;
 }
 
-// Workspace for this shape and every smaller max_seq_len: the splits do not fall with it.
+// Workspace for this shape and every smaller max_seq_len: a shorter bound may take the other kind of row tiles, with as many splits as
+// compute units leave it.
 static size_t prompt_scratch_bytes(const ygg_shape& s) {
-    const PromptPlan p = plan_prompt(s);
-    return p.part_o_bytes + p.part_rec_bytes;
+    if (s.kv_dtype == YGG_F32) return 0;
+    const int64_t G = s.n_q_heads / s.n_kv_heads, rows = s.n_nodes * G, each = (rows + s.batch - 1) / s.batch;
+    const int64_t tiles = (s.max_seq_len + kKeyTile - 1) / kKeyTile;
+    int64_t most = 1;
+    for (int64_t tile : {128, 256}) {
+        const int64_t groups = (each + tile - 1) / tile * std::min((int64_t)s.batch, rows) * s.n_kv_heads;
+        most = std::max(most, std::clamp(std::min(256 / groups, tiles / 4), (int64_t)1, (int64_t)32));
+    }
+    return most > 1 ? prompt_part_o_bytes(s, most) + prompt_part_rec_bytes(s, most) : 0;
 }
 
 // Raises the shared-memory limits of the current device's kernels once; later calls cost one atomic load.
