@@ -367,7 +367,8 @@ int32_t ygg_tree_rotary(const ygg_shape *shape, const void *q, int64_t q_stride,
  * The same rotation behind a norm of every head, in one pass over q and k: with x a head's values of one token and w its weights,
  *     y_d = x_d * w_d / sqrt(sum_d x_d^2 / head_dim + eps)   in fp32, not rounded; then the pairs of y as above, rounded once
  *   q_weight, k_weight [Dh] fp32 device, or [Hq,Dh] and [Hkv,Dh] if weights_per_head, 16-byte aligned; needed with their tensor
- *   eps          finite, >= 0.  (A head of zeros is 0 also with eps = 0.)  The sum of the squares must stay below fp32's largest value
+ *   eps          finite, >= 0.  The sum of a head's squares must stay below fp32's largest value; a head whose mean square and eps
+ *                together are below 2^-126 (zeros, with eps = 0) comes out as zeros
  * Everything else as for ygg_tree_rotary.
  */
 int32_t ygg_tree_norm_rotary(const ygg_shape *shape, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
@@ -390,7 +391,8 @@ int32_t ygg_tree_norm_rotary(const ygg_shape *shape, const void *q, int64_t q_st
  *   q, out [n_nodes,Hq,Dh];  k, v [kv_capacity,Hkv,Dh];  lse [n_nodes,Hq] fp32 or NULL.  Rows of q, k and v are q_stride, k_stride and
  *                v_stride elements apart (0: dense), so that parts of a fused projection can be given; out is dense and overlaps nothing
  *   q_first, q_len, k_first, k_len [B] int32 device.  No two sequences share rows of q; they may share keys.  A sequence that does not
- *                lie inside the rows is cut to those that do, and k_len to max_seq_len.  Rows of out and lse of no sequence are not written
+ *                lie inside the rows is cut to those that do, and k_len to max_seq_len.  Rows of out and lse of no sequence are not written.
+ *                A sequence's q, k and v are finite, with finite scores; what lies outside of the sequences may be anything
  * Workspace: ygg_workspace_bytes(PROMPT_ATTENTION), which may be 0; what serves max_seq_len serves every smaller one.
  */
 int32_t ygg_prompt_attention(const ygg_shape *shape, const void *q, int64_t q_stride, const void *k, int64_t k_stride,

@@ -896,7 +896,8 @@ int32_t ygg_prompt_attention(const ygg_shape* s, const void* q, int64_t q_stride
         return YGG_ERR_UNSUPPORTED;
     if (k_stride > (1 << 24) || v_stride > (1 << 24)) return YGG_ERR_UNSUPPORTED;   // (32-bit offsets inside a tile of keys)
     const PromptPlan p = plan_prompt(*s);
-    if ((int64_t)p.ranks * s->n_kv_heads * p.splits > (1 << 22) || (int64_t)p.merge_ranks * s->n_kv_heads > (1 << 23)) return YGG_ERR_UNSUPPORTED;   // (the launch grid)
+    if ((int64_t)p.ranks * s->n_kv_heads * p.splits > (1 << 22) || (p.splits > 1 && (int64_t)p.merge_ranks * s->n_kv_heads > (1 << 23)))
+        return YGG_ERR_UNSUPPORTED;   // (the launch grid)
     if (int32_t rc = check_workspace(workspace, workspace_bytes, prompt_scratch_bytes(*s))) return rc;
     if (int32_t rc = ensure_device_ready()) return rc;
     PromptArgs a{};

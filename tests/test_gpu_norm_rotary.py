@@ -100,6 +100,16 @@ def test_heads_of_zeros_and_of_any_magnitude(dtype):
         assert (out[0, 0] == 0).all()
 
 
+def test_a_head_whose_squares_are_subnormal_counts_as_zeros():
+    q = torch.ones((1, 4, 2, 128), device=DEV)
+    q[0, 0], q[0, 1], q[0, 2] = 2.0 ** -62, 2.0 ** -64, 1e-45
+    out = torch.full_like(q, float("nan"))
+    w = torch.ones(128, device=DEV)
+    pos = torch.zeros((1, 4), dtype=torch.int32, device=DEV)
+    ygg.tree_norm_rotary(_shape(1, 4, 2, 2, 128, ygg.F32), q, None, out, None, w, None, ygg.rotary_frequencies(64).to(DEV), positions=pos, eps=0.0)
+    assert (out[0, [0, 3]] == 1).all() and (out[0, [1, 2]] == 0).all()
+
+
 def test_the_norm_of_ones_is_the_rotation_alone():
     shape = _shape(2, 9, 4, 2, 128, ygg.F32)
     q = torch.sign(torch.randn((2, 9, 4, 128), device=DEV))        # every head's mean square is 1
