@@ -345,7 +345,11 @@ BlockPlan plan_block(const ygg_shape& s, int bits) {
     const int64_t rounds = (groups + slots - 1) / slots;
     const float whole = unit * (float)(rounds * (longest + 4));
     const float stream = 2.f * (float)s.batch * (float)s.max_seq_len * (float)Hkv * (float)s.head_dim / 5.2e6f;   // us
-    if (whole < unit * (float)best + 4.5f || (groups <= 256 && longest <= 72 && whole < stream)) {
+    // Units of the 4-bit cache are short enough for that second workgroup to show: runs -> a workgroup to each, one token behind 16 x 1024 tokens
+    // 18.0 -> 15.4 us, 13 nodes behind 4 x 2048 on 40 kv heads 25.6 -> 20.4, 17 behind 3 x 1024 on 12 of 64 11.8 -> 10.6; the runs that stay:
+    // one token behind 2048 12.4 (16.1 in one workgroup), behind 16 x 8192 38.8 (43.0), 17 nodes behind 8 x 2048 26.8 (35.0).
+    const bool shared = bits == 4 && per_cu == 2 && (int64_t)p.runs * p.row_tiles * Hkv > 256;
+    if (whole < unit * (float)best * (shared ? 1.5f : 1.f) + 4.5f || (groups <= 256 && longest <= 72 && whole < stream)) {
         p.runs = p.rem_runs = 0;
         // with a compute unit to itself a workgroup takes twice the wavefronts, unless there is little to deal out to them (one token and 367
         // tokens for 16 requests 14.2 -> 11.9 us, five nodes behind 5 x 627 18.1 -> 14.9; 61 behind 3 x 139 would go 14.6 -> 16.6)
