@@ -8,7 +8,13 @@
 // An operand in 8 bits holds its 32 values of a lane as 16 and 16 of either half of the 64 that a product sums, one in 4 bits a half as a
 // whole: q is loaded to match, and V's tokens are stored to match the scores in the accumulator.
 //
-// Half the bytes per block of the 8-bit cache leave less in flight: four stages of tiles instead of two, filled three steps ahead.
+// Half the bytes per block of the 8-bit cache leave less in flight: where row blocks share tiles four stages of them instead of two, filled
+// three steps ahead.  One row block has four wavefronts to itself and two stages: with two wavefronts and four stages 30.2 us, so 28.6, for
+// one token for 16 requests of 512 to 8192 tokens, 8 kv heads of 4 queries (2.8 TB/s; 24.9 in the main kernel, bound by the latency of a
+// run's start and of each segment's own keys, and the merge behind it).  49 nodes behind 8 x 16384 tokens on those heads: 120 us,
+// bound by the weights' vector work, 264 instructions for a wavefront's 32 rows of a tile, which overlap with the matrix pipe (48 % busy)
+// only across wavefronts.  q as two E2M3 values would take half the time on that pipe and the call 114 us, but a format of two exponent
+// bits keeps what is near the largest of 32 dimensions: a q with one large dimension would lose the others' low bits.
 #include "attn_block.h"
 
 namespace ygg {

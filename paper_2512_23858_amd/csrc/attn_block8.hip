@@ -14,11 +14,11 @@
 // The blocks of all sequences are laid end to end and cut into equal runs, one per workgroup of a (kv head, row tile), whatever the
 // lengths, with room for each sequence's own keys behind its blocks; a run is served segment by segment, one for each sequence that it
 // touches.  A segment that is all of its sequence writes the final rows; others leave a partial (m, l, O~) per row, and
-// block8_merge_kernel merges them.  Where that ends sooner each sequence is a workgroup's instead (plan_block8).
+// block_merge_kernel merges them.  Where that ends sooner each sequence is a workgroup's instead (plan_block).
 //
 // Bounds and figures: few rows are bound by the stream of codes, many by the matrix pipe and the weights' vector work beside it.  One
 // token for 16 requests of 512 to 8192 tokens, 8 kv heads of 4 queries: 35.5 us with the merge, 4.0 TB/s (the main kernel 31.4, 4.5 TB/s).
-// 49 rows behind 8 x 4096 tokens on 32 kv heads: 57.7 us, 4.9 TB/s.  1284 rows behind 32768 tokens: 160 to 177 us with the box's clock,
+// 49 rows behind 8 x 4096 tokens on 32 kv heads: 58.0 us, 4.9 TB/s.  1284 rows behind 32768 tokens: 160 to 177 us with the box's clock,
 // 0.97 to 1.08 PFLOP/s counted once (each product is two on the matrix pipe).  Row blocks to a workgroup: a tile in LDS serves all of
 // them, so as many as there are, up to eight; wavefronts that share a row block deal the tiles out.  One row block: two workgroups of two
 // wavefronts to a compute unit 40.5 us, one of four 43.7 (one token, 16 requests).

@@ -53,6 +53,7 @@ __device__ __forceinline__ void store8(T* p, const Vec8& v) {
 
 // NORM: every head is scaled by its weights and the reciprocal of its root mean square first.  A head's units are neighbouring lanes, so
 // the sum of its squares meets in four or eight of them; a unit's weights come as its values do, and from L1 after the first token.
+// 2 x 6000 tokens of 40 heads of 128, interleaved pairs in half of each: 51.2 us, 4.8 TB/s; 49 nodes for 16 requests of 72 heads 8.5 us, a chain of latencies; one token 2.4.
 template <typename T, bool INTERLEAVED, bool NORM>
 __global__ __launch_bounds__(kTokens * 64) void rotary_kernel(RotaryArgs a) {
     __shared__ int32_t parent_s[kMaxNodes];
