@@ -84,15 +84,18 @@ __device__ __forceinline__ Tile find_tile(const PromptArgs& a, int rank, int row
 }
 
 // NW wavefronts of 32 rows.  PHASES (eight wavefronts): the two wavefronts of a SIMD are held half a block apart by a barrier between any
-// two phases, so that one has the matrix pipe while the other forms its weights; it takes a fourth tile buffer.
+// two phases, so that one has the matrix pipe while the other forms its weights; it takes a fourth tile buffer.  The launch bound of two wavefronts
+// to a SIMD also holds where four would do with one: above 256 registers matrix results go to accumulation registers, and are copied from
+// there for the vector instructions, 48 copies to 42 of these at head_dim 64 (eight prompts of 90 to 2047 tokens 41.9 us, so 38.6).
 template <int DH, int NW, bool PHASES>
-__global__ __launch_bounds__(NW * 64, NW / 4) void prompt_kernel(PromptArgs a) {
+__global__ __launch_bounds__(NW * 64, 2) void prompt_kernel(PromptArgs a) {
     constexpr int ROWB = 2 * DH;                 // bytes of a row in LDS
     constexpr int NS = DH / 16, NDB = DH / 32;   // steps of S^T, blocks of O^T
     constexpr int SLOTS = ROWB / 16, RPI = 1024 / ROWB;   // 16-byte slots of a row; rows of a direct load
     constexpr int RW = NW * 32, TILEB = kKeys * ROWB, NBUF = PHASES ? 4 : 3;
     constexpr int PT = 2 * (kKeys / RPI) / NW;   // direct loads of a wavefront per tile: K's and V's in turn
-    static_assert(RPI * NW % SLOTS == 0 && PT % 2 == 0, "a wavefront's rows of a tile share their place in the permutation");
+    constexpr int SH = DH == 64 ? 1 : 0;         // two rows of 128 bytes lie side by side in the banks: the slots go by pairs of rows
+    static_assert(RPI * NW % (SLOTS << SH) == 0 && PT % 2 == 0, "a wavefront's rows of a tile share their place in the permutation");
     extern __shared__ __align__(16) unsigned char smem[];
     unsigned char* const k_s = smem;
     unsigned char* const v_s = smem + NBUF * TILEB;
@@ -145,7 +148,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void prompt_kernel(PromptArgs a) {
         const unsigned char* const vb = uniform_ptr(static_cast<const unsigned char*>(a.v) + (k0 * a.v_stride + g * DH) * 2);
         const uint32_t k_tok = (uint32_t)a.k_stride * 2, v_tok = (uint32_t)a.v_stride * 2;
         const int fill_row = RPI * wave + lane / SLOTS;
-        const uint32_t k_slot = 16 * ((lane % SLOTS) ^ (fill_row & (SLOTS - 1))), v_slot = 16 * ((lane % SLOTS) ^ ((fill_row & (NDB - 1)) << 2));
+        const uint32_t k_slot = 16 * ((lane % SLOTS) ^ (fill_row >> SH & (SLOTS - 1))), v_slot = 16 * ((lane % SLOTS) ^ ((fill_row >> SH & (NDB - 1)) << 2));
         const uint32_t fill_k = fill_row * k_tok + k_slot, fill_v = fill_row * v_tok + v_slot;
         const uint32_t k_lds = uniform((uint32_t)(size_t)(__attribute__((address_space(3))) void*)k_s + wave * 1024);
         auto fill = [&](auto from, auto to, int buf, int key) __attribute__((always_inline)) {
@@ -170,8 +173,8 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void prompt_kernel(PromptArgs a) {
         auto fill_tile = [&](int t) { if (t < ntiles) fill(IntC<0>{}, IntC<PT>{}, t % NBUF, base + t * kKeys); };
 
         const int j16 = lane & 15;
-        const int k_lane = n * ROWB + 16 * (g2 ^ (n & 1)), k_xor = ((n & (SLOTS - 1)) >> 1) << 5;
-        const int v_row = 4 * g2 + (j16 >> 2), v_lane = v_row * ROWB + 8 * (j16 & 3), v_pair = (lane >> 4) & 1, v_xor = (v_row & (NDB - 1)) << 1;
+        const int k_lane = n * ROWB + 16 * (g2 ^ (n >> SH & 1)), k_xor = ((n >> SH & (SLOTS - 1)) >> 1) << 5;
+        const int v_row = 4 * g2 + (j16 >> 2), v_lane = v_row * ROWB + 8 * (j16 & 3), v_pair = (lane >> 4) & 1, v_xor = (v_row >> SH & (NDB - 1)) << 1;
         auto read_k = [&](int buf, int half, bf16x8 (&ka)[NS]) {
             const unsigned char* const p = k_s + buf * TILEB + half * 32 * ROWB + k_lane;
 #pragma unroll
@@ -463,7 +466,7 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PromptArgs a) {
 // summed values a step takes is free: of the head's dimensions 8 c + 4 half + 0 .. 3 in four steps, so that K comes in reads of 16 bytes, and
 // of the keys the two that a score register holds in the two halves, so that the weights are operands as they lie.
 template <int DH>
-__global__ __launch_bounds__(256) void prompt_f32_kernel(PromptArgs a) {
+__global__ __launch_bounds__(256, 2) void prompt_f32_kernel(PromptArgs a) {
     constexpr int KT = 32, PITCH = DH + 4, RW = 128, NDB = DH / 32, NC = DH / 8;
     __shared__ __align__(16) float k_s[KT * PITCH], v_s[KT * PITCH];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), n = lane & 31, half = lane >> 5;
