@@ -373,15 +373,16 @@ static size_t prompt_part_o_bytes(const ygg_shape& s, int64_t splits) { return a
 static size_t prompt_part_rec_bytes(const ygg_shape& s, int64_t splits) { return align256((size_t)splits * s.n_nodes * s.n_q_heads * sizeof(float3)); }
 
 // Workgroups and key splits of the attention of prompts: row tiles of 256 or of 128 rows, and where these leave compute units without work
-// their keys in parts.  The kind of least estimated time, from a start and a time per tile of 64 keys (us, fitted): 256 rows take as long per
-// tile as 128 at head_dim 128, where either has its compute unit to itself, but start later; at head_dim 64 three workgroups of 128 rows
-// share one.  us per call, 128 rows / 256: a prompt of 512 tokens with heads 32/8 of 128 18 / 21, of 2048 63 / 54, of 8192 718 / 462,
-// 64 of 60 tokens 37 / 29, 300 tokens behind 16000 138 / 87, 64 behind 8000 26 / 29; heads 12 of 64, eight of 90 to 2047 tokens 41.5 / 45.5,
-// 32/8 of 64, of 4096 tokens 107 / 93.  Without parts: 64 tokens behind 8000 185, 16 behind 30000 (heads 64/8) 680 (with: 26 and 40).
+// their keys in parts.  The kind of least estimated time, from a start and a time per tile of 64 keys (us, fitted): 256 rows take little
+// longer per tile than 128 at head_dim 128, where either has its compute unit to itself, but start later; at head_dim 64 three workgroups of
+// 128 rows share one.  us per call, 128 rows / 256: a prompt of 512 tokens with heads 32/8 of 128 17 / 21, of 1024 26 / 32, of 2048 57 / 53, of
+// 4096 187 / 134, eight of 300 29 / 24, 300 tokens behind 16000 115 / 85, 64 behind 8000 23 / 28; heads 12 of 64, 2048 tokens 31 / 32, eight of
+// 2000 70 / 89, 700 behind 3000 26 / 24; 32/8 of 64, 4096 tokens 84 / 92.  Without parts: 64 tokens behind 8000 185, 16 behind 30000 (heads
+// 64/8) 680 (with: 23 and 35).
 PromptPlan plan_prompt(const ygg_shape& s) {
     struct Kind { int32_t waves; float start, tile, shared; int64_t at_once; };   // shared: time per tile of a workgroup among several
-    static constexpr Kind kinds128[] = {{4, 10.f, 1.15f, 1.15f, 256}, {8, 14.f, 1.25f, 1.25f, 256}};
-    static constexpr Kind kinds64[] = {{4, 8.f, 0.95f, 0.72f, 768}, {8, 13.f, 1.15f, 1.15f, 256}};
+    static constexpr Kind kinds128[] = {{4, 9.f, 1.05f, 1.15f, 256}, {8, 14.f, 1.25f, 1.25f, 256}};
+    static constexpr Kind kinds64[] = {{4, 5.f, 0.85f, 0.6f, 768}, {8, 11.f, 1.15f, 1.15f, 256}};
     PromptPlan p{};
     const int64_t G = s.n_q_heads / s.n_kv_heads, rows = s.n_nodes * G, Hkv = s.n_kv_heads;
     const bool f32 = s.kv_dtype == YGG_F32;
@@ -393,14 +394,16 @@ PromptPlan plan_prompt(const ygg_shape& s) {
     float least = 0.f;
     for (const Kind& k : s.head_dim == 128 ? kinds128 : kinds64) {
         const int64_t tile = 32 * k.waves, groups = (each + tile - 1) / tile * std::min((int64_t)s.batch, rows) * Hkv;
-        const int64_t splits = f32 ? 1 : std::clamp(std::min(256 / groups, tiles / 4), (int64_t)1, (int64_t)32);
-        const float time = k.start * (float)((groups * splits + k.at_once - 1) / k.at_once) +
-                           std::max(k.tile * (float)((tiles + splits - 1) / splits), k.shared * mean * (float)groups / 256.f) +
-                           (splits > 1 ? 4.f + 0.1f * (float)splits : 0.f);
-        if (p.waves == 0 || (time < least && !f32)) {
-            least = time;
-            p.waves = k.waves;
-            p.splits = (int32_t)splits;
+        const int64_t most = f32 ? 1 : std::clamp(std::min(256 / groups, tiles / 4), (int64_t)1, (int64_t)32);
+        for (const int64_t splits : {(int64_t)1, most}) {   // (parts cost a merge: 512 tokens with heads 12 of 64 in two 13 us, in one 11)
+            const float time = k.start * (float)((groups * splits + k.at_once - 1) / k.at_once) +
+                               std::max(k.tile * (float)((tiles + splits - 1) / splits), k.shared * mean * (float)groups / 256.f) +
+                               (splits > 1 ? 4.f + 0.1f * (float)splits : 0.f);
+            if (p.waves == 0 || (time < least && !f32)) {
+                least = time;
+                p.waves = k.waves;
+                p.splits = (int32_t)splits;
+            }
         }
     }
     const int64_t tile = 32 * p.waves;

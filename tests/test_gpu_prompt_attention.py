@@ -114,7 +114,9 @@ def test_chunks_behind_cached_keys_and_queries_that_see_nothing(dtype, Dh, heads
 
 PLANS = [  # heads, Dh, q_lens, k_lens, (rows of a workgroup, key splits > 1)
     ((32, 8), 128, [1500, 1, 300], None, (256, False)), ((40, 40), 128, [1000, 700], None, (256, False)),
-    ((40, 8), 128, [600], [9000], (256, True)), ((32, 8), 128, [990], None, (256, True)), ((12, 12), 64, [1990], None, (256, True)),
+    ((40, 8), 128, [600], [9000], (256, True)), ((32, 8), 128, [990], None, (128, False)), ((12, 12), 64, [1990], None, (128, False)),
+    ((32, 8), 128, [990], [1900], (256, True)), ((12, 12), 64, [150, 149, 140, 100], [2150, 2000, 1900, 300], (256, True)),
+    ((32, 8), 64, [100] * 16, [9000] + [300] * 15, (256, False)),
     ((64, 8), 128, [30, 77], [3000, 2500], (256, True)), ((8, 8), 128, [4100], None, (128, False)), ((8, 8), 64, [4100], None, (128, False)),
     ((32, 32), 64, [700, 699], None, (128, False)), ((8, 8), 128, [40] * 20, None, (128, False)), ((8, 1), 128, [600], None, (128, True)),
     ((2, 2), 64, [600, 300], None, (128, True)), ((8, 1), 128, [16], [5000], (128, True)), ((4, 4), 64, [3, 1], [5000, 70], (128, True)),
@@ -134,9 +136,9 @@ def test_the_bound_may_be_far_above_the_lengths():
     p = _problem((8, 2), 128, [20, 3], [100, 40], seed=1, k_gap=9000, most=18000)
     assert ygg.prompt_plan(p["shape"])["splits"] > 1
     _check(p, *_attend(p))
-    # rows of no sequence count too: tiles of 256 rows at head_dim 64
+    # rows of no sequence count too: tiles of 256 rows
     for lens in ([700], [200, 70]):
-        p = _problem((40, 40), 64, lens, seed=2, gap=(3000 - sum(lens)) // (len(lens) + 1), most=3000 // len(lens) - 20)
+        p = _problem((40, 40), 128, lens, seed=2, gap=(3000 - sum(lens)) // (len(lens) + 1), most=3000 // len(lens) - 20)
         if len(lens) == 1:
             assert (ygg.prompt_plan(p["shape"])["rows"], ygg.prompt_plan(p["shape"])["splits"]) == (256, 1)
         _check(p, *_attend(p))
