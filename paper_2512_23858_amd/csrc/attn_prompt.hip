@@ -83,6 +83,11 @@ __device__ __forceinline__ Tile find_tile(const PromptArgs& a, int rank, int row
     return {-1, 0};
 }
 
+// Tile buffers.  Four wavefronts: so few that two workgroups have room on a compute unit at head_dim 128 (with three buffers and one workgroup
+// 4096 tokens, heads 32/8, take 189 us, so 149), and three at 64.
+template <int DH, bool PHASES>
+constexpr int kBuffers = PHASES ? 4 : DH == 128 ? 2 : 3;
+
 // NW wavefronts of 32 rows.  PHASES (eight wavefronts): the two wavefronts of a SIMD are held half a block apart by a barrier between any
 // two phases, so that one has the matrix pipe while the other forms its weights; it takes a fourth tile buffer.  The launch bound of two wavefronts
 // to a SIMD also holds where four would do with one: above 256 registers matrix results go to accumulation registers, and are copied from
@@ -92,7 +97,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_kernel(PromptArgs a) {
     constexpr int ROWB = 2 * DH;                 // bytes of a row in LDS
     constexpr int NS = DH / 16, NDB = DH / 32;   // steps of S^T, blocks of O^T
     constexpr int SLOTS = ROWB / 16, RPI = 1024 / ROWB;   // 16-byte slots of a row; rows of a direct load
-    constexpr int RW = NW * 32, TILEB = kKeys * ROWB, NBUF = PHASES ? 4 : 3;
+    constexpr int RW = NW * 32, TILEB = kKeys * ROWB, NBUF = kBuffers<DH, PHASES>;
     constexpr int PT = 2 * (kKeys / RPI) / NW;   // direct loads of a wavefront per tile: K's and V's in turn
     constexpr int SH = DH == 64 ? 1 : 0;         // two rows of 128 bytes lie side by side in the banks: the slots go by pairs of rows
     static_assert(RPI * NW % (SLOTS << SH) == 0 && PT % 2 == 0, "a wavefront's rows of a tile share their place in the permutation");
@@ -254,7 +259,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_kernel(PromptArgs a) {
         fill_tile(1);
         if (ntiles > 1) dma_wait_keep<PT>(); else dma_wait_keep<0>();
         lds_barrier();
-        fill_tile(2);
+        if constexpr (NBUF > 2) fill_tile(2);
         read_k(0, 0, ka);
         if constexpr (PHASES) read_v(0, 0, va);
         qk(ka, s);
@@ -334,9 +339,9 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_kernel(PromptArgs a) {
                 read_v(buf, 1, va);
                 __builtin_amdgcn_sched_barrier(0);
                 softmax(s, p, key + 32, key + 64 <= clean);
-                if (t + 2 < ntiles) dma_wait_keep<PT>(); else dma_wait_keep<0>();   // tile t + 1 is here, t + 2 may be under way
+                if (NBUF > 2 && t + 2 < ntiles) dma_wait_keep<PT>(); else dma_wait_keep<0>();   // tile t + 1 is here, t + 2 may be under way
                 lds_barrier();
-                if (t + 3 < ntiles) fill(IntC<0>{}, IntC<PT>{}, buf, key + 3 * kKeys);
+                if (t + NBUF < ntiles) fill(IntC<0>{}, IntC<PT>{}, buf, key + NBUF * kKeys);
                 if (more) read_k(next, 0, ka);
                 __builtin_amdgcn_sched_barrier(0);
                 pv(va, p);
@@ -565,7 +570,7 @@ __global__ __launch_bounds__(256, 2) void prompt_f32_kernel(PromptArgs a) {
 }
 
 template <int DH, int NW, bool PHASES>
-constexpr int kSmem = 2 * (PHASES ? 4 : 3) * kKeys * 2 * DH;
+constexpr int kSmem = 2 * kBuffers<DH, PHASES> * kKeys * 2 * DH;
 
 template <int DH, int NW, bool PHASES>
 hipError_t raise() {

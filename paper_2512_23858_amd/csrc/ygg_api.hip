@@ -373,16 +373,27 @@ static size_t prompt_part_o_bytes(const ygg_shape& s, int64_t splits) { return a
 static size_t prompt_part_rec_bytes(const ygg_shape& s, int64_t splits) { return align256((size_t)splits * s.n_nodes * s.n_q_heads * sizeof(float3)); }
 
 // Workgroups and key splits of the attention of prompts: row tiles of 256 or of 128 rows, and where these leave compute units without work
-// their keys in parts.  The kind of least estimated time, from a start and a time per tile of 64 keys (us, fitted): 256 rows take little
-// longer per tile than 128 at head_dim 128, where either has its compute unit to itself, but start later; at head_dim 64 three workgroups of
-// 128 rows share one.  us per call, 128 rows / 256: a prompt of 512 tokens with heads 32/8 of 128 17 / 21, of 1024 26 / 32, of 2048 57 / 53, of
-// 4096 187 / 134, eight of 300 29 / 24, 300 tokens behind 16000 115 / 85, 64 behind 8000 23 / 28; heads 12 of 64, 2048 tokens 31 / 32, eight of
-// 2000 70 / 89, 700 behind 3000 26 / 24; 32/8 of 64, 4096 tokens 84 / 92.  Without parts: 64 tokens behind 8000 185, 16 behind 30000 (heads
-// 64/8) 680 (with: 23 and 35).
+// their keys in parts.  The kind of least estimated time, from a start and a time per tile of 64 keys (us, fitted): 256 rows take as long per
+// tile as 128 where either has its compute unit to itself, but start later, and two (head_dim 64: three) workgroups of 128 rows share one.
+// us per call, 128 rows / 256: a prompt of 512 tokens with heads 32/8 of 128 15 / 21, of 2048 52 / 55, of 4096 149 / 137, of 8192 513 / 474, eight
+// of 300 23 / 24, 64 of 60 24 / 29, 300 tokens behind 16000 97 / 84, 64 behind 8000 24 / 28; heads 12 of 64, 2048 tokens 24 / 32, eight of 2000
+// 70 / 90, 700 behind 3000 27 / 25; 32/8 of 64, 4096 tokens 85 / 96.
+// Without parts: 64 tokens behind 8000 185, 16 behind 30000 (heads 64/8) 680 (with: 23 and 35).
+struct PromptKind {
+    int32_t waves;
+    float start, tile, shared;   // shared: time per tile of a workgroup among several
+    int64_t at_once;             // workgroups on the chip
+};
+static const PromptKind* prompt_kinds(int head_dim) {
+    static constexpr PromptKind of128[] = {{4, 6.f, 1.25f, 1.02f, 512}, {8, 14.f, 1.25f, 1.25f, 256}};
+    static constexpr PromptKind of64[] = {{4, 5.f, 0.85f, 0.6f, 768}, {8, 11.f, 1.15f, 1.15f, 256}};
+    return head_dim == 128 ? of128 : of64;
+}
+static int64_t most_prompt_splits(const PromptKind& k, int64_t groups, int64_t tiles) {
+    return std::clamp(std::min(k.at_once / groups, tiles / 4), (int64_t)1, (int64_t)32);
+}
+
 PromptPlan plan_prompt(const ygg_shape& s) {
-    struct Kind { int32_t waves; float start, tile, shared; int64_t at_once; };   // shared: time per tile of a workgroup among several
-    static constexpr Kind kinds128[] = {{4, 9.f, 1.05f, 1.15f, 256}, {8, 14.f, 1.25f, 1.25f, 256}};
-    static constexpr Kind kinds64[] = {{4, 5.f, 0.85f, 0.6f, 768}, {8, 11.f, 1.15f, 1.15f, 256}};
     PromptPlan p{};
     const int64_t G = s.n_q_heads / s.n_kv_heads, rows = s.n_nodes * G, Hkv = s.n_kv_heads;
     const bool f32 = s.kv_dtype == YGG_F32;
@@ -392,18 +403,24 @@ PromptPlan plan_prompt(const ygg_shape& s) {
     const int64_t queries = (s.n_nodes + s.batch - 1) / s.batch;
     const float mean = s.max_seq_len <= 2 * queries ? 0.5f * (float)(tiles + 1) : (float)tiles - 0.5f * (float)queries / kKeyTile;
     float least = 0.f;
-    for (const Kind& k : s.head_dim == 128 ? kinds128 : kinds64) {
+    for (int kind = 0; kind < 2; ++kind) {
+        const PromptKind& k = prompt_kinds(s.head_dim)[kind];
         const int64_t tile = 32 * k.waves, groups = (each + tile - 1) / tile * std::min((int64_t)s.batch, rows) * Hkv;
-        const int64_t most = f32 ? 1 : std::clamp(std::min(256 / groups, tiles / 4), (int64_t)1, (int64_t)32);
-        for (const int64_t splits : {(int64_t)1, most}) {   // (parts cost a merge: 512 tokens with heads 12 of 64 in two 13 us, in one 11)
-            const float time = k.start * (float)((groups * splits + k.at_once - 1) / k.at_once) +
-                               std::max(k.tile * (float)((tiles + splits - 1) / splits), k.shared * mean * (float)groups / 256.f) +
-                               (splits > 1 ? 4.f + 0.1f * (float)splits : 0.f);
+        const int64_t most = f32 ? 1 : most_prompt_splits(k, groups, tiles);
+        // parts: a merge, and partial rows written and read (512 tokens with heads 32/8 of 128 in two 17 us, in one 15)
+        for (int64_t splits = most;; splits = splits / 2) {
+            const int64_t all = groups * splits;
+            const float share = all <= k.at_once ? (float)((all + 255) / 256) : (float)all / 256.f;   // workgroups that a compute unit gets
+            const float mb = 2e-6f * (float)(splits * rows * Hkv * s.head_dim);
+            const float time = k.start * (float)((all + k.at_once - 1) / k.at_once) +
+                               std::max(k.tile * (float)((tiles + splits - 1) / splits), k.shared * mean / (float)splits * share) +
+                               (splits > 1 ? 4.f + 0.1f * (float)splits + 0.4f * mb : 0.f);
             if (p.waves == 0 || (time < least && !f32)) {
                 least = time;
                 p.waves = k.waves;
                 p.splits = (int32_t)splits;
             }
+            if (splits == 1) break;
         }
     }
     const int64_t tile = 32 * p.waves;
@@ -426,9 +443,10 @@ static size_t prompt_scratch_bytes(const ygg_shape& s) {
     const int64_t G = s.n_q_heads / s.n_kv_heads, rows = s.n_nodes * G, each = (rows + s.batch - 1) / s.batch;
     const int64_t tiles = (s.max_seq_len + kKeyTile - 1) / kKeyTile;
     int64_t most = 1;
-    for (int64_t tile : {128, 256}) {
-        const int64_t groups = (each + tile - 1) / tile * std::min((int64_t)s.batch, rows) * s.n_kv_heads;
-        most = std::max(most, std::clamp(std::min(256 / groups, tiles / 4), (int64_t)1, (int64_t)32));
+    for (int kind = 0; kind < 2; ++kind) {
+        const PromptKind& k = prompt_kinds(s.head_dim)[kind];
+        const int64_t tile = 32 * k.waves, groups = (each + tile - 1) / tile * std::min((int64_t)s.batch, rows) * s.n_kv_heads;
+        most = std::max(most, most_prompt_splits(k, groups, tiles));
     }
     return most > 1 ? prompt_part_o_bytes(s, most) + prompt_part_rec_bytes(s, most) : 0;
 }

@@ -113,14 +113,14 @@ def test_chunks_behind_cached_keys_and_queries_that_see_nothing(dtype, Dh, heads
 
 
 PLANS = [  # heads, Dh, q_lens, k_lens, (rows of a workgroup, key splits > 1)
-    ((32, 8), 128, [1500, 1, 300], None, (256, False)), ((40, 40), 128, [1000, 700], None, (256, False)),
-    ((40, 8), 128, [600], [9000], (256, True)), ((32, 8), 128, [990], None, (128, False)), ((12, 12), 64, [1990], None, (128, False)),
-    ((32, 8), 128, [990], [1900], (256, True)), ((12, 12), 64, [150, 149, 140, 100], [2150, 2000, 1900, 300], (256, True)),
-    ((32, 8), 64, [100] * 16, [9000] + [300] * 15, (256, False)),
-    ((64, 8), 128, [30, 77], [3000, 2500], (256, True)), ((8, 8), 128, [4100], None, (128, False)), ((8, 8), 64, [4100], None, (128, False)),
-    ((32, 32), 64, [700, 699], None, (128, False)), ((8, 8), 128, [40] * 20, None, (128, False)), ((8, 1), 128, [600], None, (128, True)),
-    ((2, 2), 64, [600, 300], None, (128, True)), ((8, 1), 128, [16], [5000], (128, True)), ((4, 4), 64, [3, 1], [5000, 70], (128, True)),
-    ((1, 1), 128, [1], [9999], (128, True)), ((12, 12), 64, [100, 200], [4000, 30], (128, True)),
+    ((32, 8), 128, [1500, 1, 300], None, (256, False)), ((40, 8), 128, [600], [9000], (256, True)),
+    ((12, 12), 128, [150, 140, 160], [5150, 5000, 300], (256, True)), ((12, 12), 64, [700] * 8, [2700] + [700] * 7, (256, False)),
+    ((8, 1), 64, [300], [30300], (256, True)), ((40, 40), 128, [1000, 700], None, (128, False)), ((8, 8), 128, [4100], None, (128, False)),
+    ((32, 32), 64, [700, 699], None, (128, False)), ((8, 8), 128, [40] * 20, None, (128, False)), ((2, 2), 64, [600, 300], None, (128, False)),
+    ((32, 8), 128, [990], None, (128, False)), ((32, 8), 128, [990], [1900], (128, True)), ((64, 8), 128, [30, 77], [3000, 2500], (128, True)),
+    ((8, 8), 64, [4100], None, (128, True)), ((12, 12), 64, [1990], None, (128, True)), ((8, 1), 128, [600], None, (128, True)),
+    ((12, 12), 64, [150, 149, 140, 100], [2150, 2000, 1900, 300], (128, True)), ((8, 1), 128, [16], [5000], (128, True)),
+    ((4, 4), 64, [3, 1], [5000, 70], (128, True)), ((1, 1), 128, [1], [9999], (128, True)), ((12, 12), 64, [100, 200], [4000, 30], (128, True)),
 ]
 
 
