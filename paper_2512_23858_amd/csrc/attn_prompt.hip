@@ -5,14 +5,12 @@
 // of 64 keys through LDS.  S^T = K Q^T with a lane per row, O^T += V^T P^T, where P's layout as an operand is that of the scores in the
 // accumulator.  Row tiles are dealt out by falling position in their sequence, whatever the batch, so that the long ones start first.
 //
-// Bounds and figures.  Long prompts are bound by the matrix pipe and, at head_dim 64, by the exponentials beside it (one per two products
-// of 64): 8192 tokens, heads 32/8 of 128: 462 to 481 us, 1.14 to 1.19 PFLOP/s (a large library product reaches 1.24).  Two wavefronts to a
-// SIMD in opposite phases (256 rows) against two that drift (128 rows): 462 against 718, as vector and matrix instructions of one wavefront
-// hardly overlap; four wavefronts of 32 rows with both kinds interleaved by hand in one stream also took 718.  500 and 333 tokens
-// behind 30000 and 15000, heads 64/8: 625 to 655 us, 27 row tiles on the 32 compute units that a kv head has, and the clock
-// makes up for most of the five that idle (the keys of all in eight parts: 640).  Eight prompts of 90 to 2047
-// tokens, heads 12 of 64: 41.9 us, as long as the longest prompt's last rows take over their 32 tiles.  A short call is a start, the chain
-// of a row tile, and a merge where the keys are in parts.
+// Bounds and figures.  Long prompts are bound by the matrix pipe and, at head_dim 64, by the vector instructions beside it (an exponential
+// goes with two products of 64): 8192 tokens, heads 32/8 of 128: 462 to 485 us, 1.13 to 1.19 PFLOP/s (a large library product reaches 1.24).
+// Two wavefronts to a SIMD in opposite phases (256 rows) take 474 there, two workgroups that drift (128 rows) 513.  500 and 333 tokens behind 30000 and 15000, heads 64/8: 625 to
+// 655 us, 27 row tiles on the 32 compute units that a kv head has, and the clock makes up for most of the five that idle (the keys of all in
+// eight parts: 640).  Eight prompts of 90 to 2047 tokens, heads 12 of 64: 38.1 us, as long as the longest prompt's last rows take over their
+// 32 tiles.  A short call is a start, the chain of a row tile, and a merge where the keys are in parts.
 #include "attn_common.h"
 
 #include <algorithm>
