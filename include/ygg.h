@@ -368,7 +368,7 @@ int32_t ygg_tree_rotary(const ygg_shape *shape, const void *q, int64_t q_stride,
  *     y_d = x_d * w_d / sqrt(sum_d x_d^2 / head_dim + eps)   in fp32, not rounded; then the pairs of y as above, rounded once
  *   q_weight, k_weight [Dh] fp32 device, or [Hq,Dh] and [Hkv,Dh] if weights_per_head, 16-byte aligned; needed with their tensor
  *   eps          finite, >= 0.  The sum of a head's squares must stay below fp32's largest value; a head whose mean square and eps
- *                together are below 2^-126 (zeros, with eps = 0) comes out as zeros
+ *                together are below 2^-126 (zeros, with eps = 0) comes out as zeros, one with a NaN as NaN throughout
  * Everything else as for ygg_tree_rotary.
  */
 int32_t ygg_tree_norm_rotary(const ygg_shape *shape, const void *q, int64_t q_stride, const void *k, int64_t k_stride,

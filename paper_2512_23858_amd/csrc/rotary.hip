@@ -110,7 +110,7 @@ __global__ __launch_bounds__(kTokens * 64) void rotary_kernel(RotaryArgs a) {
             for (int e = 0; e < 8; ++e) sum = fmaf(x.x[e], x.x[e], fmaf(y.x[e], y.x[e], sum));
             sum = group_reduce(sum, per_head, [](float p, float q) { return p + q; });   // (a head's lanes are all here or none)
             const float mean = fmaf(sum, a.Dh == 128 ? 0x1p-7f : 0x1p-6f, a.eps);
-            const float by = mean >= 0x1p-126f ? rsqrtf(mean) : 0.f;   // (subnormal squares have lost the head's values)
+            const float by = mean < 0x1p-126f ? 0.f : rsqrtf(mean);   // (subnormal squares have lost the head's values; a NaN is the whole head's)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 x.x[e] *= by * wx.x[e];

@@ -110,6 +110,28 @@ def test_a_head_whose_squares_are_subnormal_counts_as_zeros():
     assert (out[0, [0, 3]] == 1).all() and (out[0, [1, 2]] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", [ygg.F32, ygg.BF16])
+@pytest.mark.parametrize("inter", [False, True])
+def test_a_head_with_a_nan_is_nan_and_its_neighbours_are_not(dtype, inter):
+    """x / sqrt(mean(x^2)) of a head with a NaN is NaN throughout.  Everything else comes out as without it, bit for bit."""
+    dt = torch.float32 if dtype == ygg.F32 else torch.bfloat16
+    for Dh, rd in ((64, 32), (128, 128)):
+        shape = _shape(1, 9, 3, 3, Dh, dtype)
+        x = torch.randn((1, 9, 3, Dh), device=DEV).to(dt)
+        f, w = ygg.rotary_frequencies(rd).to(DEV), torch.rand(Dh, device=DEV) + 0.5
+        pos = torch.arange(9, dtype=torch.int32, device=DEV)[None]
+        run = lambda x, out: ygg.tree_norm_rotary(shape, x, None, out, None, w, None, f, positions=pos, interleaved=inter)
+        clean = torch.empty_like(x)
+        run(x, clean)
+        for at in (0, rd - 1, Dh - 1):
+            y, out = x.clone(), torch.empty_like(x)
+            y[0, 4, 1, at] = float("nan")
+            run(y, out)
+            assert out[0, 4, 1].isnan().all()
+            out[0, 4, 1] = clean[0, 4, 1]
+            assert torch.equal(out, clean)
+
+
 def test_the_norm_of_ones_is_the_rotation_alone():
     shape = _shape(2, 9, 4, 2, 128, ygg.F32)
     q = torch.sign(torch.randn((2, 9, 4, 128), device=DEV))        # every head's mean square is 1
