@@ -81,6 +81,15 @@ __device__ __forceinline__ Tile find_tile(const PromptArgs& a, int rank, int row
     return {-1, 0};
 }
 
+constexpr float kCoarse = 0x1p24f;   // references from here on, in base-2 units, are whole numbers
+
+// s * scale - against; rounded: the product is rounded first.
+__device__ __forceinline__ float less(float s, float scale, float against, bool rounded) {
+#pragma clang fp contract(off)
+    const float product = s * scale;
+    return rounded ? product - against : fmaf(s, scale, -against);
+}
+
 // Tile buffers.  Four wavefronts: so few that two workgroups have room on a compute unit at head_dim 128 (with three buffers and one workgroup
 // 4096 tokens, heads 32/8, take 189 us, so 149), and three at 64.
 template <int DH, bool PHASES>
@@ -133,6 +142,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_kernel(PromptArgs a) {
     float ref = limit > 0 ? -INFINITY : 0.f;     // (a row that sees nothing has weights of zero to any reference)
     float l = 0.f;
     const float scale = a.scale * kLog2e;
+    float most = kWeightSumLimit;                // what a lane's weights of a block may sum to without a look at the maximum
 
     if (ntiles > 0) {
         bf16x8 q[NS];
@@ -206,21 +216,24 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_kernel(PromptArgs a) {
                     o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, va[d][m]), __builtin_bit_cast(bf16x8, p[m]), o[d], 0, 0, 0);
         };
         // Weights against a reference that moves only when a block's sum past 2^30, as in the tree's kernel: no maximum on the common path.
+        // The product of score and scale is exact within the multiply-add, and a reference is such a product rounded, so the largest score is off from
+        // its own reference by up to half a step of it.  From kCoarse that is a unit and more, and soon all of a row's weights are nothing, or
+        // infinite: there the products are rounded as well.  Wavefronts with such a row take the path with the maximum for every block.
         auto softmax = [&](f32x16& s, i16x8 (&p)[2], int key, bool all) {
             if (__builtin_expect(!all, 0)) {
                 const int left = limit - key - 4 * g2;      // this half's keys are key + 4 g2 + 8 (e / 4) + e % 4
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[e] = 8 * (e / 4) + e % 4 < left ? s[e] : -INFINITY;
             }
-            auto weights = [&](float against) __attribute__((always_inline)) {
+            auto weights = [&](float against, bool coarse) __attribute__((always_inline)) {
                 float sum = 0.f;
 #pragma unroll
                 for (int m = 0; m < 2; ++m) {
                     union { bf16x2 h[4]; i16x8 v; } w;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float x = __builtin_amdgcn_exp2f(fmaf(s[8 * m + 2 * e], scale, -against));
-                        const float y = __builtin_amdgcn_exp2f(fmaf(s[8 * m + 2 * e + 1], scale, -against));
+                        const float x = __builtin_amdgcn_exp2f(less(s[8 * m + 2 * e], scale, against, coarse));
+                        const float y = __builtin_amdgcn_exp2f(less(s[8 * m + 2 * e + 1], scale, against, coarse));
                         sum += x;
                         sum += y;
                         const f32x2 xy = {x, y};
@@ -230,8 +243,8 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_kernel(PromptArgs a) {
                 }
                 return sum;
             };
-            float sum = weights(ref);
-            if (__builtin_expect(__any(!(sum <= kWeightSumLimit)), 0)) {   // (without a reference the sum is infinite or NaN)
+            float sum = weights(ref, false);
+            if (__builtin_expect(__any(!(sum <= most)), 0)) {   // (without a reference the sum is infinite or NaN)
                 float top = s[0];
 #pragma unroll
                 for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
@@ -245,7 +258,9 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_kernel(PromptArgs a) {
                 for (int d = 0; d < NDB; ++d)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) o[d][e] *= fix;
-                sum = weights(ref == -INFINITY ? 0.f : ref);
+                const bool coarse = fabsf(ref) >= kCoarse;     // (a row that has seen no key comes here again in any case)
+                most = __any(coarse) ? -1.f : kWeightSumLimit;
+                sum = weights(ref == -INFINITY ? 0.f : ref, coarse);
             }
             l += sum;
         };
