@@ -400,7 +400,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_kernel(PromptArgs a) {
         for (int d = 0; d < NDB; ++d)
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(o[d][e]));
-        top = fmaxf(fmaxf(top, __shfl_xor(top, 32)), 1e-30f);
+        top = fmaxf(fmaxf(top, __shfl_xor(top, 32)), 0x1p-126f);   // (the smallest normal number: its reciprocal is finite)
         by = 1.f / top;
     }
     const bool there = row < R;

@@ -67,3 +67,33 @@ def test_equal_scores_of_any_size_weigh_the_same(kind, dtype, power):
         # the score, its product with the scale and log2(e), and that with ln(2): 2^-24 each of the scores, the scales' own rounding likewise
         assert (np.abs(lse[:, h] - want) <= np.abs(s * most) * 2.0 ** -21 + nk * 2.0 ** -24 + 2.0 ** -20 * (1 + np.log(nk)))[good].all(), h
     assert seen_rows > 0.5 * nq * heads[0]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", [ygg.BF16, ygg.F32])
+@pytest.mark.parametrize("power", [-60, -100, -119])
+def test_small_values_keep_their_bits(kind, dtype, power):
+    """Rows whose softmax is one key or a few, values of 2^power: as exact, relative to themselves, as values of 1, with keys in parts too."""
+    heads, Dh, nq, nk, plan = kind
+    p = _kind(*kind, dtype, seed=5)
+    p["q"] = p["q"] * 30
+    p["v"] = p["v"] * 2.0 ** power
+    out, _ = (to_f64(x) for x in _attend(p))
+    q, k, v = to_f64(p["q"]), to_f64(p["k"]), to_f64(p["v"])
+    scale = p["shape"].softmax_scale
+    seen = np.arange(nk)[None] <= np.arange(nq)[:, None] + nk - nq
+    for h in range(0, heads[0], max(heads[0] // 2, 1)):
+        kv = h // (heads[0] // heads[1])
+        s = np.where(seen, q[:, h] @ k[:, kv].T * scale, -np.inf)
+        w = np.exp(s - s.max(1, keepdims=True))
+        w /= w.sum(1, keepdims=True)
+        ref, mag = w @ v[:, kv], w @ np.abs(v[:, kv])
+        # Scores: Dh rounded additions (bf16: sixteen products to an instruction, Dh / 16 + 4) of 2^-23 of the terms' magnitudes, the base-2
+        # score once more, the exponential to 2^-22; on either side of the quotient
+        terms = scale * np.abs(q[:, h]).sum(-1).max() * np.abs(k[:, kv]).max()
+        score = terms * ((Dh if dtype == ygg.F32 else Dh / 16 + 4) * 2.0 ** -23 + 2.0 ** -22) + 2.0 ** -22
+        # a product of a weight and a value, or a value of a partial row, below the smallest normal number may count as zero
+        lost = np.minimum(w * np.abs(v[:, kv]).max(), 2.0 ** -126).sum(1, keepdims=True) + 2.0 ** -126
+        tol = _out_tolerance(dtype, ref, mag, nk, plan[1]) + mag * 2 * score + lost
+        err = np.abs(out[:, h] - ref)
+        assert (err <= tol).all(), (h, (err / tol).max())
