@@ -392,7 +392,8 @@ int32_t ygg_tree_norm_rotary(const ygg_shape *shape, const void *q, int64_t q_st
  *                v_stride elements apart (0: dense), so that parts of a fused projection can be given; out is dense and overlaps nothing
  *   q_first, q_len, k_first, k_len [B] int32 device.  No two sequences share rows of q; they may share keys.  A sequence that does not
  *                lie inside the rows is cut to those that do, and k_len to max_seq_len.  Rows of out and lse of no sequence are not written.
- *                A sequence's q, k and v are finite, with finite scores; what lies outside of the sequences may be anything
+ *                A sequence's q, k and v are finite, below 2^60 in magnitude, with scores softmax_scale * q . k below 2^126 (fp32, to 2^-24 of a
+ *                score; sums of weights and values are not normalised before their end); what lies outside of the sequences may be anything
  * Workspace: ygg_workspace_bytes(PROMPT_ATTENTION), which may be 0; what serves max_seq_len serves every smaller one.
  */
 int32_t ygg_prompt_attention(const ygg_shape *shape, const void *q, int64_t q_stride, const void *k, int64_t k_stride,

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2512_23858_amd as ygg
+import plain_prompt as plain
 from gpu_util import DEV, to_f64
 from test_gpu_prompt_attention import _attend, _problem
 
@@ -97,3 +98,30 @@ def test_small_values_keep_their_bits(kind, dtype, power):
         tol = _out_tolerance(dtype, ref, mag, nk, plan[1]) + mag * 2 * score + lost
         err = np.abs(out[:, h] - ref)
         assert (err <= tol).all(), (h, (err / tol).max())
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", [ygg.BF16, ygg.F32])
+def test_values_near_2_to_the_60_under_rising_scores(kind, dtype):
+    """Every key's score is a little above the one before, by 29 base-2 units from the first to the last of a block, so that a reference lags
+    as far as it may; values all of one sign, up to 2^60."""
+    heads, Dh, nq, nk, plan = kind
+    p = _kind(*kind, dtype, seed=3)
+    t = p["k"].dtype
+    g = np.random.default_rng(4)
+    # one dimension carries the score: base-2 units (k rises by whole units and falls back every 30 keys, by 8 further units every 300)
+    j = np.arange(nk)
+    units = j % 30 + 8.0 * (j // 300 % 8)
+    k = torch.zeros((nk, heads[1], Dh), dtype=torch.float64)
+    k[:, :, 0] = torch.from_numpy(units)[:, None]
+    q = torch.zeros((nq, heads[0], Dh), dtype=torch.float64)
+    q[:, :, 0] = 1
+    p["shape"].softmax_scale = float(np.float32(np.log(2.0)))
+    p["q"], p["k"] = q.to(t).to(DEV), k.to(t).to(DEV)
+    p["v"] = torch.from_numpy((0.5 + 0.498 * g.random((nk, heads[1], Dh))) * 2.0 ** 60).to(t).to(DEV)
+    out, lse = (to_f64(x) for x in _attend(p))
+    ref, ref_lse, size = plain.prompt_attention(to_f64(p["q"]), to_f64(p["k"]), to_f64(p["v"]), p["shape"].softmax_scale)
+    # scores to 93 units, rounded with their scale to 2^-23 each: 2^-15 of a weight, on either side of the quotient
+    tol = _out_tolerance(dtype, ref, size, nk, plan[1]) + size * 2.0 ** -14
+    assert (np.abs(out - ref) <= tol).all(), (np.abs(out - ref) / tol).max()
+    assert (np.abs(lse - ref_lse) <= 2.0 ** -15 + nk * 2.0 ** -24 + 2.0 ** -20 * (1 + np.abs(ref_lse))).all()
