@@ -385,13 +385,16 @@ int32_t ygg_tree_norm_rotary(const ygg_shape *shape, const void *q, int64_t q_st
  * A query that sees no key (q_len > k_len) gets zeros, and -inf as lse.  Scores, softmax and accumulation are fp32; with bf16 the softmax
  * weights are rounded to bf16 for the value product.
  *
- *   shape        kv_dtype YGG_F32 or YGG_BF16; batch = sequences; n_nodes = rows of q and out, those of all sequences together (any
- *                number up to 2^25); kv_capacity = rows of k and v; max_seq_len = a bound of k_len, at most kv_capacity; depth, width
- *                and vocab are not read
+ *   shape        kv_dtype YGG_F32 or YGG_BF16; batch = sequences; n_nodes = rows of q and out, those of all sequences together, up to 2^25;
+ *                kv_capacity = rows of k and v, below 2^31; max_seq_len = a bound of k_len, at most kv_capacity and 2^30; depth, width and
+ *                vocab are not read.  n_nodes * n_q_heads + 128 * batch * n_kv_heads up to 2^29 is accepted, more may be refused
  *   q, out [n_nodes,Hq,Dh];  k, v [kv_capacity,Hkv,Dh];  lse [n_nodes,Hq] fp32 or NULL.  Rows of q, k and v are q_stride, k_stride and
- *                v_stride elements apart (0: dense), so that parts of a fused projection can be given; out is dense and overlaps nothing
- *   q_first, q_len, k_first, k_len [B] int32 device.  No two sequences share rows of q; they may share keys.  A sequence that does not
- *                lie inside the rows is cut to those that do, and k_len to max_seq_len.  Rows of out and lse of no sequence are not written.
+ *                v_stride elements apart (0: dense; k's and v's at most 2^24), so that parts of a fused projection can be given; out is dense
+ *                and overlaps nothing
+ *   q_first, q_len, k_first, k_len [B] int32 device.  No two sequences share rows of q; they may share keys.  Of a sequence that
+ *                ends behind the rows those that exist are taken, of keys max_seq_len at most; one that begins outside of them (a negative
+ *                first too) or whose length is negative has none.  What sees what goes by the lengths that this leaves: the last query left
+ *                sees every key left.  Rows of out and lse of no sequence are not written.
  *                A sequence's q, k and v are finite, below 2^60 in magnitude, with scores softmax_scale * q . k below 2^126 (fp32, to 2^-24 of a
  *                score; sums of weights and values are not normalised before their end); what lies outside of the sequences may be anything
  * Workspace: ygg_workspace_bytes(PROMPT_ATTENTION), which may be 0; what serves max_seq_len serves every smaller one.

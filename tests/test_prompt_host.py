@@ -148,6 +148,24 @@ def test_prompt_plan_has_a_tile_for_every_row():
                     assert (-(-lens * G // rows)).sum() <= p["tiles"], (heads, B, n)
 
 
+def test_prompts_up_to_the_stated_size_are_accepted_and_larger_ones_refused():
+    """The launch grid: row tiles of all kv heads, in as many parts as their keys have, up to 2^22."""
+    g = np.random.default_rng(0)
+    for _ in range(3000):
+        kv = int(np.exp2(g.uniform(0, 7)))
+        hq, B = kv * int(g.integers(1, 9)), int(min(np.exp2(g.uniform(0, 16)), 65535, (1 << 28) // (128 * kv)))
+        most = ((1 << 29) - 128 * B * kv) // hq
+        n = min(most, 1 << 25, int(np.exp2(g.uniform(0, 25)))) if g.random() < 0.7 else min(most, 1 << 25)
+        L = int(np.exp2(g.uniform(0, 30)))
+        s = _prompt(batch=B, n_q_heads=hq, n_kv_heads=kv, n_nodes=n, kv_capacity=L, max_seq_len=L, head_dim=int(g.choice([64, 128])),
+                    kv_dtype=int(g.choice([ygg.BF16, ygg.F32])))
+        p = ygg.prompt_plan(s)
+        assert p["tiles"] * kv * p["splits"] <= 1 << 22, (s, p)
+    good = [FAKE, 0, FAKE, 0, FAKE, 0, FAKE, FAKE, FAKE, FAKE, FAKE, None, FAKE, BIG]
+    for kw in (dict(n_nodes=1 << 25, n_q_heads=32, n_kv_heads=32), dict(batch=65535, n_q_heads=512, n_kv_heads=512, n_nodes=1 << 20)):
+        assert _call("ygg_prompt_attention", _prompt(**kw), good) == UNSUPPORTED, kw
+
+
 def test_cache_tensors_and_storage_order():
     c = ygg.new_block4_cache(_shape(head_dim=64, kv_capacity=201), 3, device="cpu")
     assert isinstance(c, ygg.Block4Cache) and isinstance(c.layer(0), ygg.Block4Cache)
