@@ -12,7 +12,8 @@
 // three steps ahead.  One row block has four wavefronts to itself and two stages: with two wavefronts and four stages 30.2 us, so 28.6, for
 // one token for 16 requests of 512 to 8192 tokens, 8 kv heads of 4 queries (2.8 TB/s; 24.9 in the main kernel, bound by the latency of a
 // run's start and of each segment's own keys, and the merge behind it).  49 nodes behind 8 x 16384 tokens on those heads: 120 us,
-// bound by the weights' vector work, 264 instructions for a wavefront's 32 rows of a tile, which overlap with the matrix pipe (48 % busy)
+// 30 to 33 by the operations at these instructions' rate (3.2 to 3.5 PFLOP/s with random operands) and twice that for q's and the weights' two terms; bound
+// by the weights' vector work, 264 instructions for a wavefront's 32 rows of a tile, which overlap with the matrix pipe (48 % busy)
 // only across wavefronts.  q as two E2M3 values would take half the time on that pipe and the call 114 us, but a format of two exponent
 // bits keeps what is near the largest of 32 dimensions: a q with one large dimension would lose the others' low bits.
 #include "attn_block.h"

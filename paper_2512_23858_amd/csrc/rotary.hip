@@ -3,8 +3,8 @@
 // A wavefront takes one token, or a part of its heads where there are few tokens.  Its lanes first form the token's angles, one pair
 // each: the turn p * f / 2 pi in fp64 (at position 10^6 an fp32 angle is off by 0.03 radians), its fraction of a whole turn, then
 // sine and cosine of that in fp32.  Then a lane takes units of eight pairs -- two pieces of 16 bytes (fp32: 32) that lie half the
-// rotated part apart, or next to each other where pairs are interleaved -- so that no value has to change lanes.  Bound by the stream
-// of q and k; the unrotated part of a head passes through the same units.  2 x 8191 tokens of 40 heads of 128, bf16: 68.2 us, 4.9 TB/s, a
+// rotated part apart, or half a head apart where pairs are interleaved -- so that no value has to change lanes.  Bound by the stream
+// of q and k; the unrotated part of a head passes through the same units, in two pieces side by side, or half a head apart likewise.  2 x 8191 tokens of 40 heads of 128, bf16: 68.2 us, 4.9 TB/s, a
 // copy's rate (past the caches it takes 81); 49 nodes for 16 requests of 72 heads 7.3 us; one token 2.2.
 #include "ygg_internal.h"
 #include "ygg_device.h"
