@@ -323,7 +323,8 @@ typedef struct {
  *   q, out [B,N,Hq,Dh] bf16;  k_tree, v_tree [B,N,Hkv,Dh] bf16;  lse [B,N,Hq] fp32 or NULL;  seq_lens, parent_idx int32
  * q (bf16, 8 bits of significand) and the softmax weights enter the products as sums of two E4M3 values, that is with 8 bits and
  * an exponent per row and tile; softmax and accumulation are fp32 (the matrix instructions of 8-bit values cut each product at
- * 2^-13 of the largest of its group before they add).  Workspace: ygg_workspace_bytes(ATTENTION_BLOCK8).
+ * 2^-13 of the largest of its group before they add).  A weight below 2^-126 of its row's largest may count as that much.
+ * Workspace: ygg_workspace_bytes(ATTENTION_BLOCK8).
  */
 int32_t ygg_tree_attention_block8(const ygg_shape *shape, const void *q, const ygg_block8_cache *cache /* host struct */,
                                   const int32_t *seq_lens, const void *k_tree, const void *v_tree,
